@@ -293,6 +293,41 @@ int rope_rotate(const seco_desc* desc, int32_t n_heads, const void* x_in, void* 
                 float rope_base, int32_t inverse, void* hip_stream);
 
 /*
+ * Layer norm of rows, with an optional residual add in front, and its backward (operators of the models that the chunk calls
+ * are used in; not part of the paper).  Rows have d elements, d of any size, contiguous; the strides between rows are given.
+ * Pointers need the alignment of their elements only.  Statistics, sums and products are fp32; a result is rounded once.
+ *   forward    s = x, or x + residual rounded to dtype (written to x_out);  mean, var of a row of s;
+ *              rstd = 1 / sqrt(var + eps);  y = (s - mean) * rstd * gain + bias
+ *   backward   n = (x - mean) * rstd, e = d_y * gain:  d_x = d_in + rstd * (e - mean(e) - n * mean(e * n)),
+ *              d_gain = sum over rows of d_y * n,  d_bias = sum over rows of d_y   (fixed order: reproducible)
+ * gain, bias   [d] of gain_dtype, or NULL (ones, zeros)
+ * mean, rstd   fp32 [rows], one behind the other
+ * residual and x_out go together, both or neither; x_out may be x or residual, y may be x when there is no residual (same
+ * stride).  d_in may be NULL (nothing is added); d_x may be x, d_y or d_in (same stride).  In the backward, x is the row that
+ * was normalised: x_out where there was a residual.  d_gain, d_bias: overwritten; NULL: not wanted.
+ * rows = 0 is allowed (d_gain and d_bias are then zeros).  Row strides of inputs may be 0 (one row for all).
+ * ws of the backward: layer_norm_workspace_bytes(desc) bytes, 16-byte aligned; not needed when neither d_gain nor d_bias is
+ * wanted.
+ */
+typedef struct layer_norm_desc {
+  int64_t rows, d;
+  int64_t x_stride;         /* x */
+  int64_t residual_stride;  /* residual, d_in */
+  int64_t out_stride;       /* x_out, d_x */
+  int64_t y_stride;         /* y, d_y */
+  int32_t dtype;            /* seco_dtype of x, residual, x_out, y, d_y, d_in, d_x */
+  int32_t gain_dtype;       /* of gain, bias, d_gain, d_bias: dtype or SECO_F32 */
+  float eps;                /* >= 0, finite (SECO_ERR_RANGE) */
+} layer_norm_desc;
+int layer_norm_fwd(const layer_norm_desc* desc, const void* x, const void* residual, const void* gain, const void* bias,
+                   void* x_out, void* y, float* mean, float* rstd, void* hip_stream);
+int layer_norm_bwd(const layer_norm_desc* desc, const void* x, const void* gain, const float* mean, const float* rstd,
+                   const void* d_y, const void* d_in, void* d_x, void* d_gain, void* d_bias, void* ws, size_t ws_bytes,
+                   void* hip_stream);
+/* (size_t)-1 for an invalid desc */
+size_t layer_norm_workspace_bytes(const layer_norm_desc* desc);
+
+/*
  * SpaCO chunk selection (Alg. 2, selection step: t different chunks out of k, uniformly), host only.
  * Deterministic in (seed, step): SplitMix64 stream keyed by (seed, step), unbiased bounded
  * draws by rejection, first t steps of a Fisher-Yates shuffle of 0..k-1, result sorted in

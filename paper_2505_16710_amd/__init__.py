@@ -11,6 +11,8 @@ from .binding import (  # noqa: F401
     kvgrad_accumulate,
     kvgrad_readout,
     kvgrad_zero,
+    layer_norm_bwd,
+    layer_norm_fwd,
     library_path,
     load_library,
     rope_rotate,

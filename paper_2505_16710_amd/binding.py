@@ -235,6 +235,21 @@ def rope_rotate(x, pos_start, rope_base, inverse=False, out=None, stream=None):
     return (_ext or _load_ext()).rotate(x, pos_start, rope_base, inverse, out, stream)
 
 
+def layer_norm_fwd(x, gain=None, bias=None, eps=1e-5, residual=None, y=None, x_out=None, stream=None):
+    """Layer norm of the rows of x [..., d] (bf16 or fp32; rows contiguous, at one distance from each other).
+    Returns (y, mean, rstd), mean and rstd fp32 [...]; with a residual (shape and dtype of x) that is added first, (y, mean,
+    rstd, x_out) with x_out = x + residual, rounded.  gain, bias: [d] of x's dtype or fp32, or None.  y may be x without a
+    residual, x_out may be x or residual."""
+    return (_ext or _load_ext()).norm_fwd(x, gain, bias, eps, residual, y, x_out, stream)
+
+
+def layer_norm_bwd(x, gain, mean, rstd, d_y, d_in=None, d_x=None, with_gain=True, with_bias=True, ws=None, stream=None):
+    """Backward of layer_norm_fwd: (d_x, d_gain, d_bias), the last two [d] of the gain's dtype (of x's without a gain), None
+    where with_gain / with_bias is false.  x: what was normalised (x_out where there was a residual).  d_in (shape of x), if
+    given, is added to d_x: the gradient that reaches the rows past the norm.  d_x may be x, d_y or d_in."""
+    return (_ext or _load_ext()).norm_bwd(x, gain, mean, rstd, d_y, d_in, d_x, with_gain, with_bias, ws, stream)
+
+
 def spaco_select_chunks(seed, step, k, t):
     """t distinct chunk indices of 0..k-1, descending (list of int)."""
     out = (C.c_int32 * max(int(t), 1))()

@@ -25,7 +25,8 @@ using at::Tensor;
   X(seco_workspace_bytes) X(kvgrad_zero) X(kvgrad_accumulate) X(kv_append) X(kvgrad_readout) X(kv_append_rope)      \
   X(kvgrad_readout_rope) X(rope_rotate) X(dec_add_rmsnorm) X(dec_rmsnorm_bwd) X(dec_silu) X(dec_silu_bwd)             \
   X(dec_cross_entropy) X(dec_cross_entropy_both) X(dec_embedding_bwd) X(dec_gemm_supported) X(dec_gemm) X(dec_gemm_grads) X(dec_gemm_first_grads)      \
-  X(dec_rope_qkv) X(dec_gemm_qkv) X(dec_gain_sums) X(dec_split_columns) X(dec_embed_rmsnorm_checked)
+  X(dec_rope_qkv) X(dec_gemm_qkv) X(dec_gain_sums) X(dec_split_columns) X(dec_embed_rmsnorm_checked)              \
+  X(layer_norm_fwd) X(layer_norm_bwd) X(layer_norm_workspace_bytes)
 struct Lib {
 #define X(name) decltype(&::name) name = nullptr;
   SECO_ENTRIES(X)
@@ -154,5 +155,6 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define SECO_METHOD(name, f, n) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&seco_ext::entry<f, n>)), METH_FASTCALL, nullptr}
 
 extern PyMethodDef step_methods[];   // the training step (chunk_step_ext.cpp)
+extern PyMethodDef train_methods[];  // the operators around it (train_ops_ext.cpp)
 
 }  // namespace seco_ext

@@ -266,6 +266,6 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_seco_ext", "native half of the bi
 
 PyMODINIT_FUNC PyInit__seco_ext() {
   PyObject* m = PyModule_Create(&module);
-  if (m && PyModule_AddFunctions(m, seco_ext::step_methods) < 0) Py_CLEAR(m);
+  if (m && (PyModule_AddFunctions(m, seco_ext::step_methods) < 0 || PyModule_AddFunctions(m, seco_ext::train_methods) < 0)) Py_CLEAR(m);
   return m;
 }

@@ -1,0 +1,605 @@
+// Layer norm.  Forward: s = x + r (rounded to the rows' type where there is a residual r), mean and variance of a row of s,
+// y = (s - mean) rstd gain + bias.  Backward, with n = (x - mean) rstd and e = dy gain:
+//   d_x = d_in + rstd (e - mean(e) - n mean(e n)),   d_gain = sum over rows of dy n,   d_bias = sum over rows of dy.
+//
+// Bound by memory: every row is read once and held in registers from the first sum to the result; all of a row's loads are
+// issued before the first is used.  A group of G lanes takes a row: 16 lanes for the shortest (four rows to a wavefront), a
+// wavefront where the row fits its registers (no barrier then), a workgroup beyond.
+// Sums are fp32 in a fixed order.  The variance is taken about the mean (a second pass over registers): with
+// m0 the rounded mean, delta = mean(s - m0) corrects it, so that rows with a mean far from zero keep their precision.
+#include <type_traits>
+
+#include "row_tiles.h"
+#include "train_ops.h"
+
+namespace seco {
+namespace {
+
+constexpr int kBlock = 512;                    // threads of a workgroup that takes a row
+constexpr int64_t kGridX = 1 << 22;            // workgroups along x: a launch holds fewer than 2^32 threads in a dimension
+
+// Where a group's lane finds its k-th word of a row of d elements: at `at`, with the elements from `skip` on its own.  The
+// last word of a row whose length is no multiple of V overlaps the one in front of it (both lanes then store the
+// same values there); behind the end there are none (skip = V).
+template <int V, int G> struct Place {
+  unsigned at;
+  int skip;
+  __device__ __forceinline__ Place(int k, int lane, int d) {
+    const int c = (k * G + lane) * V;
+    at = (unsigned)(c + V <= d ? c : d - V);
+    skip = c < d ? c - (int)at : V;
+  }
+};
+// The row's number where all lanes of a wavefront share it: its address is then a scalar
+template <int G> __device__ __forceinline__ int64_t row_of(int64_t row) {
+  if constexpr (G < 64) return row;
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)row), hi = __builtin_amdgcn_readfirstlane((unsigned)(row >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+template <typename T, int V> __device__ __forceinline__ void load_gain(const void* p, bool f32, unsigned at, float* g) {
+  if (sizeof(T) == 4 || f32)
+    Pack<float, V>::at(static_cast<const float*>(p), at).get(g);
+  else
+    Pack<T, V>::at(static_cast<const T*>(p), at).get(g);
+}
+
+// Where a lane finds its KB words, and the gain there in fp32 (ones without one)
+template <typename T, int V, int G, int KB> struct Words {
+  int lane, d;
+  __device__ __forceinline__ Words(int lane, int d) : lane(lane), d(d) {}
+  __device__ __forceinline__ Place<V, G> operator[](int k) const { return Place<V, G>(k, lane, d); }
+};
+template <typename T, int V, int G, int KB>
+__device__ __forceinline__ void gains(const NormArgs& a, const Words<T, V, G, KB>& at, float (&gain)[KB][V]) {
+#pragma unroll
+  for (int k = 0; k < KB; ++k) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) gain[k][j] = 1.f;
+    if (a.gain) load_gain<T, V>(a.gain, a.gain_f32, at[k].at, gain[k]);
+  }
+}
+
+// Sums over a workgroup of kBlock threads of N <= 16 values at a time, as scalars; sh: this call's own scratch until the call
+// after the next.  Behind the barrier lane i + 16 w of every wavefront adds the shares of wavefronts w and w + 4 of value i,
+// then the four lanes of a value add theirs.
+template <int N> __device__ __forceinline__ void block_sums(float (&x)[N], float (*sh)[N]) {
+  static_assert(N <= 16 && (N & (N - 1)) == 0 && kBlock == 512, "");
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = lanes_sum<64>(x[i]);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (lane == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) sh[wave][i] = x[i];
+  __syncthreads();
+  const float v = sum_across_32(sum_across_16(sh[lane >> 4][lane & (N - 1)] + sh[(lane >> 4) + 4][lane & (N - 1)]));
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i));
+}
+
+// ---- forward: G lanes to a row, KB words of V elements to a lane
+template <typename T, int V, int G, int KB>
+__global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_kernel(NormArgs a) {
+  constexpr int kRows = G > 256 ? 1 : 256 / G;
+  __shared__ float sh[2][G / 64 + 1][2];
+  const int lane = threadIdx.x % G;
+  const int64_t row = row_of<G>(((int64_t)blockIdx.y * kGridX + blockIdx.x) * kRows + threadIdx.x / G);
+  if (row >= a.rows) return;                      // (a workgroup to a row: all of it)
+  const int d = (int)a.d;
+  const T* x = static_cast<const T*>(a.x) + row * a.xs;
+  const T* r = a.r ? static_cast<const T*>(a.r) + row * a.rs : nullptr;
+  bool bad = false;
+  if (a.token) {
+    int64_t t = a.token[row];
+    t += t < 0 ? a.table : 0;
+    bad = t < 0 || t >= a.table;
+    if (bad && a.outside && lane == 0) *a.outside = 1.f;
+    x = static_cast<const T*>(a.x) + (bad ? 0 : t) * a.xs;
+  }
+  Pack<T, V> w[KB], rw[KB];
+#pragma unroll
+  for (int k = 0; k < KB; ++k) w[k] = Pack<T, V>::at(x, Place<V, G>(k, lane, d).at);
+  if (r)
+#pragma unroll
+    for (int k = 0; k < KB; ++k) rw[k] = Pack<T, V>::at(r, Place<V, G>(k, lane, d).at);
+  float f[KB][V], sum[1] = {0.f};
+#pragma unroll
+  for (int k = 0; k < KB; ++k) {
+    const Place<V, G> p(k, lane, d);
+    w[k].get(f[k]);
+    if (r) {
+      float g[V];
+      rw[k].get(g);
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[k][j] += g[j];
+      w[k] = Pack<T, V>::of(f[k]);
+      w[k].get(f[k]);
+    }
+    if (a.token && bad) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[k][j] = NAN;
+      w[k] = Pack<T, V>::of(f[k]);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[0] += j >= p.skip ? f[k][j] : 0.f;
+  }
+  if constexpr (G <= 64) sum[0] = lanes_sum<G>(sum[0]);
+  else block_sums<1>(sum, reinterpret_cast<float(*)[1]>(sh[0]));
+  const float inv = 1.f / (float)d, m0 = sum[0] * inv;
+  float two[2] = {0.f, 0.f};                      // of the deviations from m0, and of their squares
+#pragma unroll
+  for (int k = 0; k < KB; ++k) {
+    const Place<V, G> p(k, lane, d);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      f[k][j] -= m0;
+      const float dev = j >= p.skip ? f[k][j] : 0.f;
+      two[0] += dev;
+      two[1] += dev * dev;
+    }
+  }
+  if constexpr (G <= 64) {
+    two[0] = lanes_sum<G>(two[0]);
+    two[1] = lanes_sum<G>(two[1]);
+  } else {
+    block_sums<2>(two, sh[1]);
+  }
+  const float delta = two[0] * inv, var = fmaxf(two[1] * inv - delta * delta, 0.f), rstd = 1.f / sqrtf(var + a.eps);
+  if (lane == 0) {
+    a.mean[row] = m0 + delta;
+    a.rstd[row] = rstd;
+  }
+  T* y = static_cast<T*>(a.y) + row * a.ys;
+  T* out = a.out ? static_cast<T*>(a.out) + row * a.os : nullptr;
+#pragma unroll
+  for (int k = 0; k < KB; ++k) {
+    const Place<V, G> p(k, lane, d);
+    if (p.skip >= V) continue;
+    float g[V], b[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) g[j] = (f[k][j] - delta) * rstd;
+    if (a.gain) {
+      load_gain<T, V>(a.gain, a.gain_f32, p.at, b);
+#pragma unroll
+      for (int j = 0; j < V; ++j) g[j] *= b[j];
+    }
+    if (a.bias) {
+      load_gain<T, V>(a.bias, a.gain_f32, p.at, b);
+#pragma unroll
+      for (int j = 0; j < V; ++j) g[j] += b[j];
+    }
+    if (out) w[k].to(out, p.at);
+    Pack<T, V>::of(g).to(y, p.at);
+  }
+}
+
+// Rows longer than a workgroup's registers: three walks over the row (the second and third from the caches).
+template <typename T>
+__global__ __launch_bounds__(kBlock) void norm_fwd_long_kernel(NormArgs a) {
+  __shared__ float sh[2][kBlock / 64][2];
+  const int64_t row = (int64_t)blockIdx.y * kGridX + blockIdx.x, d = a.d;
+  if (row >= a.rows) return;
+  const T* x = static_cast<const T*>(a.x) + row * a.xs;
+  const T* r = a.r ? static_cast<const T*>(a.r) + row * a.rs : nullptr;
+  bool bad = false;
+  if (a.token) {
+    int64_t t = a.token[row];
+    t += t < 0 ? a.table : 0;
+    bad = t < 0 || t >= a.table;
+    if (bad && a.outside && threadIdx.x == 0) *a.outside = 1.f;
+    x = static_cast<const T*>(a.x) + (bad ? 0 : t) * a.xs;
+  }
+  T* out = a.out ? static_cast<T*>(a.out) + row * a.os : nullptr;
+  // out may lie over x or r: an element is read and written by one thread, and read again from out
+  auto first = [&](int64_t c) {
+    float f = bad ? NAN : (float)x[c];
+    if (r) f = (float)(T)(f + (float)r[c]);
+    if (out) out[c] = (T)f;
+    return f;
+  };
+  auto again = [&](int64_t c) { return out ? (float)out[c] : bad ? NAN : (float)x[c]; };
+  float sum[1] = {0.f};
+  for (int64_t c = threadIdx.x; c < d; c += kBlock) sum[0] += first(c);
+  block_sums<1>(sum, reinterpret_cast<float(*)[1]>(sh[0]));
+  const float inv = 1.f / (float)d, m0 = sum[0] * inv;
+  float two[2] = {0.f, 0.f};
+  for (int64_t c = threadIdx.x; c < d; c += kBlock) {
+    const float dev = again(c) - m0;
+    two[0] += dev;
+    two[1] += dev * dev;
+  }
+  block_sums<2>(two, sh[1]);
+  const float delta = two[0] * inv, var = fmaxf(two[1] * inv - delta * delta, 0.f), rstd = 1.f / sqrtf(var + a.eps);
+  if (threadIdx.x == 0) {
+    a.mean[row] = m0 + delta;
+    a.rstd[row] = rstd;
+  }
+  T* y = static_cast<T*>(a.y) + row * a.ys;
+  for (int64_t c = threadIdx.x; c < d; c += kBlock) {
+    float f = ((again(c) - m0) - delta) * rstd, g[1];
+    if (a.gain) {
+      load_gain<T, 1>(a.gain, a.gain_f32, (unsigned)c, g);
+      f *= g[0];
+    }
+    if (a.bias) {
+      load_gain<T, 1>(a.bias, a.gain_f32, (unsigned)c, g);
+      f += g[0];
+    }
+    y[c] = (T)f;
+  }
+}
+
+// ---- backward, G <= 64 lanes to a row: the workgroup's groups take rows in turn, each lane keeps the gain and the sums of its
+// columns; at the end they are added up over the groups through LDS, halves upon halves, and left as the workgroup's row of
+// the parts.
+template <typename T, int V, int G, int KB, bool IN>
+__global__ __launch_bounds__(kBlock) void norm_bwd_rows_kernel(NormArgs a) {
+  constexpr int kRows = kBlock / G, kWaves = kBlock / 64, kCols = G * KB * V;
+  __shared__ float sh[kWaves / 2][kCols];
+  const int lane = threadIdx.x % G, wave = threadIdx.x >> 6, d = (int)a.d;
+  const float inv = 1.f / (float)d;
+  float dg[KB][V], db[KB][V], gain[KB][V];
+  Words<T, V, G, KB> at(lane, d);
+  gains<T, V, G, KB>(a, at, gain);
+  Pack<T, V> own[KB];                             // (what is another lane's, or no row's, counts as a dy of zero)
+#pragma unroll
+  for (int k = 0; k < KB; ++k) own[k] = Pack<T, V>::from(at[k].skip);
+#pragma unroll
+  for (int k = 0; k < KB; ++k)
+#pragma unroll
+    for (int j = 0; j < V; ++j) dg[k][j] = db[k][j] = 0.f;
+  for (int64_t row = row_of<G>((int64_t)blockIdx.x * kRows + threadIdx.x / G); row < a.rows; row += (int64_t)a.blocks * kRows) {
+    const T* x = static_cast<const T*>(a.x) + row * a.xs;
+    const T* dy = static_cast<const T*>(a.dy) + row * a.ys;
+    const T* in = static_cast<const T*>(a.r) + row * a.rs;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    Pack<T, V> xw[KB], yw[KB], iw[KB];
+#pragma unroll
+    for (int k = 0; k < KB; ++k) {
+      xw[k] = Pack<T, V>::at(x, at[k].at);
+      yw[k] = Pack<T, V>::at(dy, at[k].at);
+      if constexpr (IN) iw[k] = Pack<T, V>::at(in, at[k].at);
+    }
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int k = 0; k < KB; ++k) {
+      float n[V], y[V];
+      xw[k].get(n);
+      (yw[k] & own[k]).get(y);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        n[j] = (n[j] - mean) * rstd;
+        dg[k][j] += y[j] * n[j];
+        db[k][j] += y[j];
+        s1 += y[j] * gain[k][j];
+        s2 += y[j] * gain[k][j] * n[j];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < KB; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) here(dg[k][j]), here(db[k][j]);
+    s1 = lanes_sum<G>(s1) * inv;
+    s2 = lanes_sum<G>(s2) * inv;
+    T* out = static_cast<T*>(a.out) + row * a.os;
+#pragma unroll
+    for (int k = 0; k < KB; ++k) {
+      float n[V], y[V], f[V];
+      xw[k].renew(s2);
+      yw[k].renew(s2);
+      xw[k].get(n);
+      yw[k].get(y);
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] = rstd * (y[j] * gain[k][j] - s1 - (n[j] - mean) * rstd * s2);
+      if constexpr (IN) {
+        iw[k].get(n);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] += n[j];
+      }
+      if (at[k].skip < V) Pack<T, V>::of(f).to(out, at[k].at);
+    }
+  }
+  if (!a.parts) return;
+  float* part = a.parts + (int64_t)blockIdx.x * d;
+  auto leave = [&](float (&s)[KB][V], float* to) {
+#pragma unroll
+    for (int k = 0; k < KB; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if constexpr (G == 16) s[k][j] = sum_across_32(sum_across_16(s[k][j]));
+#pragma unroll
+    for (int half = kWaves / 2; half > 0; half >>= 1) {
+      __syncthreads();
+      if (wave >= half && wave < 2 * half && (threadIdx.x & 63) < G)
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+#pragma unroll
+          for (int j = 0; j < V; ++j) sh[wave - half][(k * V + j) * G + lane] = s[k][j];
+      __syncthreads();
+      if (wave < half)
+#pragma unroll
+        for (int k = 0; k < KB; ++k)
+#pragma unroll
+          for (int j = 0; j < V; ++j) s[k][j] += sh[wave][(k * V + j) * G + lane];
+    }
+    if (threadIdx.x >= G) return;
+#pragma unroll
+    for (int k = 0; k < KB; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j >= at[k].skip) to[at[k].at + j] = (a.accumulate ? to[at[k].at + j] : 0.f) + s[k][j];
+  };
+  leave(dg, part);
+  leave(db, part + (int64_t)a.blocks * d);
+}
+
+// ---- backward, a workgroup to a row, R rows at a time: one barrier for the 2 R sums, all of their loads in flight together
+template <typename T, int V, int KB, int R, bool IN>
+__global__ __launch_bounds__(kBlock) void norm_bwd_block_kernel(NormArgs a) {
+  __shared__ float sh[2][kBlock / 64][2 * R];
+  const int d = (int)a.d;
+  const float inv = 1.f / (float)d;
+  float dg[KB][V], db[KB][V], gain[KB][V];
+  Words<T, V, kBlock, KB> at(threadIdx.x, d);
+  gains<T, V, kBlock, KB>(a, at, gain);
+  Pack<T, V> own[KB];
+#pragma unroll
+  for (int k = 0; k < KB; ++k) own[k] = Pack<T, V>::from(at[k].skip);
+#pragma unroll
+  for (int k = 0; k < KB; ++k)
+#pragma unroll
+    for (int j = 0; j < V; ++j) dg[k][j] = db[k][j] = 0.f;
+  int turn = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < a.rows; r0 += (int64_t)a.blocks * R, turn ^= 1) {
+    Pack<T, V> xw[R][KB], yw[R][KB], iw[R][KB];
+    float mean[R], rstd[R], s[2 * R];
+    const int there = (int)min((int64_t)R, a.rows - r0);      // rows of this round; the others repeat the last one
+    int64_t xs = a.xs, ys = a.ys, rs = a.rs;
+    asm volatile("" : "+s"(xs), "+s"(ys), "+s"(rs));             // (or every row's address is kept through the loop)
+    const T* x0 = static_cast<const T*>(a.x) + r0 * xs;
+    const T* dy0 = static_cast<const T*>(a.dy) + r0 * ys;
+    const T* in0 = static_cast<const T*>(a.r) + r0 * rs;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int r = min(i, there - 1);
+      const T *x = x0 + r * xs, *dy = dy0 + r * ys, *in = in0 + r * rs;
+      mean[i] = a.mean[r0 + r];
+      rstd[i] = a.rstd[r0 + r];
+#pragma unroll
+      for (int k = 0; k < KB; ++k) {
+        xw[i][k] = Pack<T, V>::at(x, at[k].at);
+        yw[i][k] = Pack<T, V>::at(dy, at[k].at);
+        if constexpr (IN) iw[i][k] = Pack<T, V>::at(in, at[k].at);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const unsigned is = i < there ? 0xffffffffu : 0u;
+      s[2 * i] = s[2 * i + 1] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KB; ++k) {
+        float n[V], y[V];
+        if (i > 0) {                             // one row's fp32 values at a time
+          xw[i][k].renew(s[2 * i - 1]);
+          yw[i][k].renew(s[2 * i - 1]);
+        }
+        xw[i][k].get(n);
+        (yw[i][k] & own[k] & is).get(y);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          n[j] = (n[j] - mean[i]) * rstd[i];
+          dg[k][j] += y[j] * n[j];
+          db[k][j] += y[j];
+          s[2 * i] += y[j] * gain[k][j];
+          s[2 * i + 1] += y[j] * gain[k][j] * n[j];
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < KB; ++k)
+#pragma unroll
+      for (int j = 0; j < V; ++j) here(dg[k][j]), here(db[k][j]);
+    block_sums<2 * R>(s, sh[turn]);
+    int64_t os = a.os;
+    asm volatile("" : "+s"(os));
+    T* out0 = static_cast<T*>(a.out) + r0 * os;
+    [[maybe_unused]] float last = s[0];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const float s1 = s[2 * i] * inv, s2 = s[2 * i + 1] * inv;
+      T* out = out0 + i * os;
+#pragma unroll
+      for (int k = 0; k < KB; ++k) {
+        float n[V], y[V], f[V];
+        xw[i][k].renew(s2);
+        yw[i][k].renew(s2);
+        xw[i][k].get(n);
+        yw[i][k].get(y);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = rstd[i] * (y[j] * gain[k][j] - s1 - (n[j] - mean[i]) * rstd[i] * s2);
+        if constexpr (IN) {
+          iw[i][k].get(n);
+#pragma unroll
+          for (int j = 0; j < V; ++j) f[j] += n[j];
+        }
+        last = f[V - 1];
+        if (i < there && at[k].skip < V) Pack<T, V>::of(f).to(out, at[k].at);
+      }
+    }
+  }
+  if (!a.parts) return;
+  float* part = a.parts + (int64_t)blockIdx.x * d;
+  float* part_b = part + (int64_t)a.blocks * d;
+#pragma unroll
+  for (int k = 0; k < KB; ++k)
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (j >= at[k].skip) {
+        float *g = part + at[k].at + j, *b = part_b + at[k].at + j;
+        *g = (a.accumulate ? *g : 0.f) + dg[k][j];
+        *b = (a.accumulate ? *b : 0.f) + db[k][j];
+      }
+}
+
+// Rows longer than that: two walks over the row; the sums of a column are kept in the workgroup's row of the parts.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void norm_bwd_long_kernel(NormArgs a) {
+  __shared__ float sh[2][kBlock / 64][2];
+  const int64_t d = a.d;
+  const float inv = 1.f / (float)d;
+  float* part = a.parts ? a.parts + (int64_t)blockIdx.x * d : nullptr;
+  float* part_b = part ? part + (int64_t)a.blocks * d : nullptr;
+  if (part && !a.accumulate)
+    for (int64_t c = threadIdx.x; c < d; c += kBlock) part[c] = part_b[c] = 0.f;     // (each element is one thread's own)
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += a.blocks, turn ^= 1) {
+    const T* x = static_cast<const T*>(a.x) + row * a.xs;
+    const T* dy = static_cast<const T*>(a.dy) + row * a.ys;
+    const T* in = a.r ? static_cast<const T*>(a.r) + row * a.rs : nullptr;
+    T* out = static_cast<T*>(a.out) + row * a.os;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    auto terms = [&](int64_t c, float& n, float& e, float& y) {
+      float g[1] = {1.f};
+      y = (float)dy[c];
+      n = ((float)x[c] - mean) * rstd;
+      if (a.gain) load_gain<T, 1>(a.gain, a.gain_f32, (unsigned)c, g);
+      e = y * g[0];
+    };
+    float s[2] = {0.f, 0.f}, n, e, y;
+    for (int64_t c = threadIdx.x; c < d; c += kBlock) {
+      terms(c, n, e, y);
+      s[0] += e;
+      s[1] += e * n;
+    }
+    block_sums<2>(s, sh[turn]);
+    for (int64_t c = threadIdx.x; c < d; c += kBlock) {
+      terms(c, n, e, y);
+      if (part) {
+        part[c] += y * n;
+        part_b[c] += y;
+      }
+      const float f = rstd * (e - s[0] * inv - n * (s[1] * inv));
+      out[c] = (T)(in ? (float)in[c] + f : f);
+    }
+  }
+}
+
+// d_gain (blockIdx.y 0) or d_bias: 32 columns to a workgroup, 32 groups of 8 lanes, each every 32nd block's share in ascending
+// order, then the groups in theirs.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_sums_kernel(const float* parts, int blocks, int64_t d, T* d_gain, T* d_bias) {
+  __shared__ float sh[32][33];
+  const float* from = parts + (int64_t)blockIdx.y * blocks * d;
+  T* to = blockIdx.y ? d_bias : d_gain;
+  if (!to) return;
+  const int group = threadIdx.x >> 3, l8 = threadIdx.x & 7;
+  const int64_t c0 = (int64_t)blockIdx.x * 32 + l8 * 4;
+  float f[4] = {0.f, 0.f, 0.f, 0.f};
+  if (c0 + 4 <= d) {
+#pragma unroll 8
+    for (int b = group; b < blocks; b += 32) {
+      float x[4];
+      Pack<float, 4>::at(from + b * d + c0).get(x);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] += x[j];
+    }
+  } else {
+    for (int b = group; b < blocks; b += 32)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c0 + j < d) f[j] += from[b * d + c0 + j];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) sh[group][l8 * 4 + j] = f[j];
+  __syncthreads();
+  const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
+  if (threadIdx.x >= 32 || c >= d) return;
+  float s = sh[0][threadIdx.x];
+#pragma unroll
+  for (int g = 1; g < 32; ++g) s += sh[g][threadIdx.x];
+  to[c] = (T)s;
+}
+
+// The kernel for rows of d elements in words of V: f is called with V, the lanes to a row and the words to a lane.
+// 16 lanes up to two words, a wavefront up to four, then a workgroup up to four.
+template <int V, typename F> bool by_length(int64_t d, F f) {
+  using std::integral_constant;
+#define SECO_NORM_CASE(G, KB)                                                                     \
+  if (d <= (G) * (KB) * V) {                                                                       \
+    f(integral_constant<int, V>{}, integral_constant<int, G>{}, integral_constant<int, KB>{});     \
+    return true;                                                                                   \
+  }
+  SECO_NORM_CASE(16, 1)
+  SECO_NORM_CASE(16, 2)
+  SECO_NORM_CASE(64, 1)
+  SECO_NORM_CASE(64, 2)
+  SECO_NORM_CASE(64, 4)
+  SECO_NORM_CASE(kBlock, 1)
+  SECO_NORM_CASE(kBlock, 2)
+  SECO_NORM_CASE(kBlock, 4)
+#undef SECO_NORM_CASE
+  return false;
+}
+// words of 16 bytes, single elements for rows shorter than that
+template <typename T, typename F> bool dispatch(int64_t d, F f) {
+  constexpr int V = 16 / sizeof(T);
+  if (d < V) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{}), true;
+  return by_length<V>(d, f);
+}
+
+dim3 rows_grid(int64_t workgroups) {
+  return dim3((unsigned)(workgroups < kGridX ? workgroups : kGridX), (unsigned)((workgroups + kGridX - 1) / kGridX));
+}
+
+template <typename T> int norm_fwd(const NormArgs& a, hipStream_t s) {
+  const bool done = dispatch<T>(a.d, [&](auto v, auto g, auto kb) {
+    constexpr int G = decltype(g)::value, kRows = G > 256 ? 1 : 256 / G;
+    hipLaunchKernelGGL((norm_fwd_kernel<T, decltype(v)::value, G, decltype(kb)::value>), rows_grid((a.rows + kRows - 1) / kRows),
+                       dim3(G > 256 ? G : 256), 0, s, a);
+  });
+  if (!done) hipLaunchKernelGGL(norm_fwd_long_kernel<T>, rows_grid(a.rows), dim3(kBlock), 0, s, a);
+  return hipGetLastError() == hipSuccess ? SECO_OK : SECO_ERR_LAUNCH;
+}
+
+constexpr int rows_at_once(int kb) { return kb == 4 ? 2 : 4; }
+template <typename T> int rows_of_block(int64_t d) {      // rows that a workgroup of the backward takes at a time
+  int n = 1;
+  dispatch<T>(d, [&](auto, auto g, auto kb) {
+    constexpr int G = decltype(g)::value;
+    n = G <= 64 ? kBlock / G : rows_at_once(decltype(kb)::value);
+  });
+  return n;
+}
+
+template <typename T> int norm_bwd(const NormArgs& a, hipStream_t s) {
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.blocks), dim3(kBlock), 0, s, a); };
+  const bool done = dispatch<T>(a.d, [&](auto v, auto g, auto kb) {
+    constexpr int V = decltype(v)::value, G = decltype(g)::value, KB = decltype(kb)::value;
+    if constexpr (G <= 64) a.r ? launch(norm_bwd_rows_kernel<T, V, G, KB, true>) : launch(norm_bwd_rows_kernel<T, V, G, KB, false>);
+    else a.r ? launch(norm_bwd_block_kernel<T, V, KB, rows_at_once(KB), true>) : launch(norm_bwd_block_kernel<T, V, KB, rows_at_once(KB), false>);
+  });
+  if (!done) hipLaunchKernelGGL(norm_bwd_long_kernel<T>, dim3(a.blocks), dim3(kBlock), 0, s, a);
+  return hipGetLastError() == hipSuccess ? SECO_OK : SECO_ERR_LAUNCH;
+}
+
+}  // namespace
+
+int norm_blocks(int64_t rows, int64_t d, int dtype) {
+  const int per = dtype == SECO_BF16 ? rows_of_block<__bf16>(d) : rows_of_block<float>(d);
+  const int64_t n = (rows + per - 1) / per;
+  return (int)(n < 1 ? 1 : n < SECO_NORM_BLOCKS ? n : SECO_NORM_BLOCKS);
+}
+
+int launch_norm_fwd(const NormArgs& a, hipStream_t s) { return a.dtype == SECO_BF16 ? norm_fwd<__bf16>(a, s) : norm_fwd<float>(a, s); }
+int launch_norm_bwd(const NormArgs& a, hipStream_t s) { return a.dtype == SECO_BF16 ? norm_bwd<__bf16>(a, s) : norm_bwd<float>(a, s); }
+
+int launch_norm_sums(const float* parts, int blocks, int64_t d, void* d_gain, void* d_bias, int gain_f32, hipStream_t s) {
+  const dim3 grid((unsigned)((d + 31) / 32), 2);
+  if (gain_f32)
+    hipLaunchKernelGGL(norm_sums_kernel<float>, grid, dim3(256), 0, s, parts, blocks, d, (float*)d_gain, (float*)d_bias);
+  else
+    hipLaunchKernelGGL(norm_sums_kernel<__bf16>, grid, dim3(256), 0, s, parts, blocks, d, (__bf16*)d_gain, (__bf16*)d_bias);
+  return hipGetLastError() == hipSuccess ? SECO_OK : SECO_ERR_LAUNCH;
+}
+
+}  // namespace seco

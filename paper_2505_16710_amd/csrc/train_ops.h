@@ -1,0 +1,37 @@
+// Host side and kernels of the operators around the training step: what the entry points (train_ops_api.cpp) hand to the
+// launchers once they have checked it.  No HIP type but the stream, so that the host side builds without a GPU compiler.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "seco.h"
+
+namespace seco {
+
+// Most workgroups of a layer norm's backward, and so most partial sums per column: one to a CU
+#define SECO_NORM_BLOCKS 256
+
+// ---- layer norm.  Row strides in elements; pointers that may be NULL are marked.
+struct NormArgs {
+  const void *x, *r;             // r: residual (forward), d_in (backward); NULL: none
+  const void *gain, *bias;       // NULL: ones, zeros
+  const void* dy;
+  void *out, *y;                 // forward: x + r (NULL without r) and the result; backward: d_x in out
+  float *mean, *rstd;
+  float *parts;                  // backward: [2][blocks][d] sums of d_gain and d_bias per workgroup, or NULL
+  int64_t rows, d, xs, rs, os, ys;
+  float eps;
+  int dtype, gain_f32;           // gain_f32: gain and bias are fp32 (else of dtype)
+  int blocks, accumulate;        // workgroups that leave sums; 1: they are added to what is there
+  // forward, first norm of a decoder: row r of x is row token[r] of a table of `table` rows
+  const int64_t* token;
+  int64_t table;
+  float* outside;
+};
+int norm_blocks(int64_t rows, int64_t d, int dtype);                       // workgroups of a backward call
+int launch_norm_fwd(const NormArgs& a, hipStream_t s);
+int launch_norm_bwd(const NormArgs& a, hipStream_t s);
+// d_gain, d_bias (either NULL) = parts added up over the blocks in their order
+int launch_norm_sums(const float* parts, int blocks, int64_t d, void* d_gain, void* d_bias, int gain_f32, hipStream_t s);
+
+}  // namespace seco

@@ -1,0 +1,162 @@
+// Binding of the operators around the training step (train_ops_api.cpp).  Third source of the extension module.
+#include <c10/core/DeviceGuard.h>
+
+#include "binding_common.h"
+
+namespace seco_ext {
+namespace {
+
+// A call's tensors are on one GPU, which is the current device while it runs; its stream, unless one is given, is that GPU's
+// current one.
+struct OnGpu {
+  c10::DeviceGuard guard;
+  void* s;
+  OnGpu(const Tensor& t, PyObject* o) : guard(t.device()), s(o == Py_None ? c10::hip::getCurrentHIPStream(t.device().index()).stream() : stream(o)) {}
+};
+void same_gpu(const Tensor& a, const Tensor& b) {
+  if (!a.is_cuda() || a.device() != b.device()) raise(PyExc_ValueError, "the tensors must be on one GPU");
+}
+
+// [..., d] seen as rows of d elements at one distance from each other
+struct Rows {
+  int64_t n = 1, d = 0, stride = 0;
+};
+Rows rows_of(const Tensor& t, const char* name) {
+  Rows r;
+  const int64_t k = t.dim();
+  if (k < 1 || t.size(k - 1) < 1 || (t.size(k - 1) > 1 && t.stride(k - 1) != 1)) {
+    PyErr_Format(PyExc_ValueError, "%s: expected [..., d] with contiguous rows of at least one element", name);
+    throw Raised{};
+  }
+  r.d = r.stride = t.size(k - 1);
+  bool even = true;
+  int64_t inner = 1;                             // rows in the dimensions behind this one
+  for (int64_t i = k - 2; i >= 0; --i) {
+    if (t.size(i) != 1) {
+      if (inner == 1) r.stride = t.stride(i);
+      else even = even && t.stride(i) == r.stride * inner;
+      inner *= t.size(i);
+    }
+  }
+  r.n = inner;
+  if (!even && r.n > 0) {
+    PyErr_Format(PyExc_ValueError, "%s: its rows must lie at one distance from each other", name);
+    throw Raised{};
+  }
+  return r;
+}
+Rows rows_like(const Tensor& t, const Tensor& x, const char* name) {
+  if (t.sizes() != x.sizes() || t.scalar_type() != x.scalar_type()) {
+    PyErr_Format(PyExc_ValueError, "%s must have the shape and dtype of x", name);
+    throw Raised{};
+  }
+  return rows_of(t, name);
+}
+void vector_of(const Tensor& t, int64_t d, at::ScalarType type, const char* name) {
+  if (t.dim() != 1 || t.size(0) != d || !t.is_contiguous() || t.scalar_type() != type) {
+    PyErr_Format(PyExc_ValueError, "%s: expected a contiguous [%lld] tensor of the gain's dtype", name, (long long)d);
+    throw Raised{};
+  }
+}
+// the type of gain and bias (none: the rows')
+at::ScalarType gain_type(const Tensor& x, const Tensor* gain, const Tensor* bias) {
+  const at::ScalarType t = gain ? gain->scalar_type() : bias ? bias->scalar_type() : x.scalar_type();
+  if (t != x.scalar_type() && t != at::kFloat) raise(PyExc_TypeError, "gain and bias must have x's dtype or float32");
+  return t;
+}
+Tensor given_or(PyObject* o, const Tensor& like_t) {
+  return o == Py_None ? at::empty(like_t.sizes(), like_t.options().requires_grad(false)) : tensor(o);
+}
+PyObject* out_ref(PyObject* o, const Tensor& t) { return o == Py_None ? THPVariable_Wrap(t) : (Py_INCREF(o), o); }
+
+layer_norm_desc norm_desc(const Tensor& x, const Rows& rows, at::ScalarType gain) {
+  layer_norm_desc d{};
+  d.rows = rows.n;
+  d.d = rows.d;
+  d.x_stride = d.residual_stride = d.out_stride = d.y_stride = rows.stride;
+  d.dtype = dtype_code(x);
+  d.gain_dtype = gain == at::kFloat ? SECO_F32 : SECO_BF16;
+  return d;
+}
+
+// (x, gain, bias, eps, residual, y, x_out, stream) -> (y, mean, rstd) or, with a residual, (y, mean, rstd, x_out)
+PyObject* norm_fwd(PyObject* const* a) {
+  const Tensor& x = tensor(a[0]);
+  const Tensor *gain = opt_tensor(a[1]), *bias = opt_tensor(a[2]), *res = opt_tensor(a[4]);
+  const Rows rows = rows_of(x, "x");
+  const at::ScalarType gt = gain_type(x, gain, bias);
+  layer_norm_desc d = norm_desc(x, rows, gt);
+  d.eps = (float)real(a[3]);
+  if (gain) vector_of(*gain, rows.d, gt, "gain");
+  if (bias) vector_of(*bias, rows.d, gt, "bias");
+  if (res) d.residual_stride = rows_like(*res, x, "residual").stride;
+  else if (a[6] != Py_None) raise(PyExc_ValueError, "x_out goes with a residual");
+  for (const Tensor* t : {gain, bias, res})
+    if (t) same_gpu(x, *t);
+  const Tensor *y_given = opt_tensor(a[5]), *out_given = opt_tensor(a[6]);
+  for (const Tensor* t : {y_given, out_given})
+    if (t) rows_like(*t, x, t == y_given ? "y" : "x_out"), same_gpu(x, *t);
+  same_gpu(x, x);
+  OnGpu on(x, a[7]);
+  const Tensor y = given_or(a[5], x);
+  Tensor out;
+  if (res) out = given_or(a[6], x);
+  const auto stats = x.options().dtype(at::kFloat).requires_grad(false);
+  const auto lead = x.sizes().slice(0, x.dim() - 1);
+  const Tensor mean = at::empty(lead, stats), rstd = at::empty(lead, stats);
+  d.y_stride = rows_of(y, "y").stride;
+  if (res) d.out_stride = rows_of(out, "x_out").stride;
+  if (rows.n > 0)
+    check(lib.layer_norm_fwd(&d, ptr(x), ptr(res), ptr(gain), ptr(bias), res ? ptr(out) : nullptr, ptr(y), fptr(mean), fptr(rstd), on.s),
+          "layer_norm_fwd");
+  if (!res) return Py_BuildValue("NNN", out_ref(a[5], y), THPVariable_Wrap(mean), THPVariable_Wrap(rstd));
+  return Py_BuildValue("NNNN", out_ref(a[5], y), THPVariable_Wrap(mean), THPVariable_Wrap(rstd), out_ref(a[6], out));
+}
+
+// (x, gain, mean, rstd, d_y, d_in, d_x, with_gain, with_bias, ws, stream) -> (d_x, d_gain or None, d_bias or None)
+PyObject* norm_bwd(PyObject* const* a) {
+  const Tensor &x = tensor(a[0]), &mean = tensor(a[2]), &rstd = tensor(a[3]), &dy = tensor(a[4]);
+  const Tensor *gain = opt_tensor(a[1]), *in = opt_tensor(a[5]), *dx_given = opt_tensor(a[6]), *ws_given = opt_tensor(a[9]);
+  const Rows rows = rows_of(x, "x");
+  const at::ScalarType gt = gain_type(x, gain, nullptr);
+  layer_norm_desc d = norm_desc(x, rows, gt);
+  if (gain) vector_of(*gain, rows.d, gt, "gain");
+  for (const Tensor* t : {&mean, &rstd})
+    if (t->scalar_type() != at::kFloat || !t->is_contiguous() || t->numel() != rows.n)
+      raise(PyExc_ValueError, "mean, rstd: contiguous float32, one value per row");
+  d.y_stride = rows_like(dy, x, "d_y").stride;
+  if (in) d.residual_stride = rows_like(*in, x, "d_in").stride;
+  if (dx_given) rows_like(*dx_given, x, "d_x");
+  for (const Tensor* t : {&mean, &rstd, &dy, gain, in, dx_given, ws_given})
+    if (t) same_gpu(x, *t);
+  const int with_gain = PyObject_IsTrue(a[7]), with_bias = PyObject_IsTrue(a[8]);
+  if (with_gain < 0 || with_bias < 0) throw Raised{};
+  OnGpu on(x, a[10]);
+  const Tensor dx = given_or(a[6], x);
+  d.out_stride = rows_of(dx, "d_x").stride;
+  const auto sums = x.options().dtype(gt).requires_grad(false);
+  Tensor dg, db, ws;
+  if (with_gain) dg = at::empty({rows.d}, sums);
+  if (with_bias) db = at::empty({rows.d}, sums);
+  if (with_gain || with_bias) {
+    const size_t n = lib.layer_norm_workspace_bytes(&d);
+    if (n == (size_t)-1) check(SECO_ERR_SHAPE, "layer_norm_workspace_bytes");
+    ws = ws_given ? *ws_given : scratch((int64_t)n, x, on.s);
+  }
+  // (an empty tensor has no address; nothing is read or written there)
+  void* some = with_gain ? ptr(dg) : with_bias ? ptr(db) : nullptr;
+  auto at_or = [&](void* p) { return p || rows.n > 0 ? p : some; };
+  if (rows.n > 0 || some)
+    check(lib.layer_norm_bwd(&d, at_or(ptr(x)), ptr(gain), static_cast<float*>(at_or(ptr(mean))), static_cast<float*>(at_or(ptr(rstd))),
+                             at_or(ptr(dy)), rows.n > 0 ? ptr(in) : nullptr, at_or(ptr(dx)), with_gain ? ptr(dg) : nullptr,
+                             with_bias ? ptr(db) : nullptr, ws.defined() ? ptr(ws) : nullptr, ws.defined() ? nbytes(ws) : 0, on.s),
+          "layer_norm_bwd");
+  auto wrap = [](const Tensor& t) { return t.defined() ? THPVariable_Wrap(t) : (Py_INCREF(Py_None), Py_None); };
+  return Py_BuildValue("NNN", out_ref(a[6], dx), wrap(dg), wrap(db));
+}
+
+}  // namespace
+
+PyMethodDef train_methods[] = {SECO_METHOD("norm_fwd", norm_fwd, 8), SECO_METHOD("norm_bwd", norm_bwd, 11), {nullptr, nullptr, 0, nullptr}};
+
+}  // namespace seco_ext
