@@ -4,7 +4,7 @@
 //
 // Bound by memory: every row is read once and held in registers from the first sum to the result; all of a row's loads are
 // issued before the first is used.  A group of G lanes takes a row: 16 lanes for the shortest (four rows to a wavefront), a
-// wavefront where the row fits its registers (no barrier then), a workgroup beyond.
+// wavefront (no barrier then), a workgroup beyond (forward_shape, backward_shape).
 // Sums are fp32 in a fixed order.  The variance is taken about the mean (a second pass over registers): with
 // m0 the rounded mean, delta = mean(s - m0) corrects it, so that rows with a mean far from zero keep their precision.
 #include <type_traits>
@@ -60,11 +60,11 @@ __device__ __forceinline__ void gains(const NormArgs& a, const Words<T, V, G, KB
   }
 }
 
-// Sums over a workgroup of kBlock threads of N <= 16 values at a time, as scalars; sh: this call's own scratch until the call
-// after the next.  Behind the barrier lane i + 16 w of every wavefront adds the shares of wavefronts w and w + 4 of value i,
-// then the four lanes of a value add theirs.
-template <int N> __device__ __forceinline__ void block_sums(float (&x)[N], float (*sh)[N]) {
-  static_assert(N <= 16 && (N & (N - 1)) == 0 && kBlock == 512, "");
+// Sums over a workgroup of TH threads of N <= 16 values at a time, as scalars; sh: this call's own scratch until the call
+// after the next.  Behind the barrier lane i + 16 w of every wavefront takes the share of wavefront w (and of w + 4) of value
+// i, then the four lanes of a value add theirs.
+template <int TH, int N> __device__ __forceinline__ void block_sums(float (&x)[N], float (*sh)[N]) {
+  static_assert(N <= 16 && (N & (N - 1)) == 0 && (TH == 256 || TH == 512), "");
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = lanes_sum<64>(x[i]);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -72,7 +72,9 @@ template <int N> __device__ __forceinline__ void block_sums(float (&x)[N], float
 #pragma unroll
     for (int i = 0; i < N; ++i) sh[wave][i] = x[i];
   __syncthreads();
-  const float v = sum_across_32(sum_across_16(sh[lane >> 4][lane & (N - 1)] + sh[(lane >> 4) + 4][lane & (N - 1)]));
+  float v = sh[lane >> 4][lane & (N - 1)];
+  if constexpr (TH == 512) v += sh[(lane >> 4) + 4][lane & (N - 1)];
+  v = sum_across_32(sum_across_16(v));
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i));
 }
@@ -80,7 +82,7 @@ template <int N> __device__ __forceinline__ void block_sums(float (&x)[N], float
 // ---- forward: G lanes to a row, KB words of V elements to a lane
 template <typename T, int V, int G, int KB>
 __global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_kernel(NormArgs a) {
-  constexpr int kRows = G > 256 ? 1 : 256 / G;
+  constexpr int kRows = G >= 256 ? 1 : 256 / G;
   __shared__ float sh[2][G / 64 + 1][2];
   const int lane = threadIdx.x % G;
   const int64_t row = row_of<G>(((int64_t)blockIdx.y * kGridX + blockIdx.x) * kRows + threadIdx.x / G);
@@ -124,7 +126,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_kernel(NormArgs a)
     for (int j = 0; j < V; ++j) sum[0] += j >= p.skip ? f[k][j] : 0.f;
   }
   if constexpr (G <= 64) sum[0] = lanes_sum<G>(sum[0]);
-  else block_sums<1>(sum, reinterpret_cast<float(*)[1]>(sh[0]));
+  else block_sums<G, 1>(sum, reinterpret_cast<float(*)[1]>(sh[0]));
   const float inv = 1.f / (float)d, m0 = sum[0] * inv;
   float two[2] = {0.f, 0.f};                      // of the deviations from m0, and of their squares
 #pragma unroll
@@ -142,7 +144,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_kernel(NormArgs a)
     two[0] = lanes_sum<G>(two[0]);
     two[1] = lanes_sum<G>(two[1]);
   } else {
-    block_sums<2>(two, sh[1]);
+    block_sums<G, 2>(two, sh[1]);
   }
   const float delta = two[0] * inv, var = fmaxf(two[1] * inv - delta * delta, 0.f), rstd = 1.f / sqrtf(var + a.eps);
   if (lane == 0) {
@@ -200,7 +202,7 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_long_kernel(NormArgs a) {
   auto again = [&](int64_t c) { return out ? (float)out[c] : bad ? NAN : (float)x[c]; };
   float sum[1] = {0.f};
   for (int64_t c = threadIdx.x; c < d; c += kBlock) sum[0] += first(c);
-  block_sums<1>(sum, reinterpret_cast<float(*)[1]>(sh[0]));
+  block_sums<kBlock, 1>(sum, reinterpret_cast<float(*)[1]>(sh[0]));
   const float inv = 1.f / (float)d, m0 = sum[0] * inv;
   float two[2] = {0.f, 0.f};
   for (int64_t c = threadIdx.x; c < d; c += kBlock) {
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_long_kernel(NormArgs a) {
     two[0] += dev;
     two[1] += dev * dev;
   }
-  block_sums<2>(two, sh[1]);
+  block_sums<kBlock, 2>(two, sh[1]);
   const float delta = two[0] * inv, var = fmaxf(two[1] * inv - delta * delta, 0.f), rstd = 1.f / sqrtf(var + a.eps);
   if (threadIdx.x == 0) {
     a.mean[row] = m0 + delta;
@@ -229,203 +231,206 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_long_kernel(NormArgs a) {
   }
 }
 
-// ---- backward, G <= 64 lanes to a row: the workgroup's groups take rows in turn, each lane keeps the gain and the sums of its
-// columns; at the end they are added up over the groups through LDS, halves upon halves, and left as the workgroup's row of
-// the parts.
-template <typename T, int V, int G, int KB, bool IN>
-__global__ __launch_bounds__(kBlock) void norm_bwd_rows_kernel(NormArgs a) {
-  constexpr int kRows = kBlock / G, kWaves = kBlock / 64, kCols = G * KB * V;
-  __shared__ float sh[kWaves / 2][kCols];
-  const int lane = threadIdx.x % G, wave = threadIdx.x >> 6, d = (int)a.d;
-  const float inv = 1.f / (float)d;
-  float dg[KB][V], db[KB][V], gain[KB][V];
-  Words<T, V, G, KB> at(lane, d);
-  gains<T, V, G, KB>(a, at, gain);
-  Pack<T, V> own[KB];                             // (what is another lane's, or no row's, counts as a dy of zero)
+// ---- backward.  A workgroup keeps the gain and the sums of its lanes' columns in registers and takes rows in turn, the next
+// ones requested before the present ones are worked on: with one workgroup to a CU nothing else covers the arithmetic.
+// What a group of lanes holds of R rows: words of x, dy and d_in, and the rows' statistics
+template <typename T, int V, int KB, int R, bool IN> struct Held {
+  Pack<T, V> x[R][KB], y[R][KB], in[IN ? R : 1][IN ? KB : 1];
+  float mean[R], rstd[R];
+  // rows r0 .. r0 + there - 1; of the others the last one again
+  template <typename At> __device__ __forceinline__ void load(const NormArgs& a, int64_t r0, int there, const At& at) {
+    int64_t xs = a.xs, ys = a.ys, rs = a.rs;
+    asm volatile("" : "+s"(xs), "+s"(ys), "+s"(rs));             // (or every row's address is kept through the loop)
+    const T* x0 = static_cast<const T*>(a.x) + r0 * xs;
+    const T* y0 = static_cast<const T*>(a.dy) + r0 * ys;
+    const T* in0 = static_cast<const T*>(a.r) + r0 * rs;
 #pragma unroll
-  for (int k = 0; k < KB; ++k) own[k] = Pack<T, V>::from(at[k].skip);
+    for (int i = 0; i < R; ++i) {
+      const int r = min(i, there - 1);
+      mean[i] = a.mean[r0 + r];
+      rstd[i] = a.rstd[r0 + r];
 #pragma unroll
-  for (int k = 0; k < KB; ++k)
-#pragma unroll
-    for (int j = 0; j < V; ++j) dg[k][j] = db[k][j] = 0.f;
-  for (int64_t row = row_of<G>((int64_t)blockIdx.x * kRows + threadIdx.x / G); row < a.rows; row += (int64_t)a.blocks * kRows) {
-    const T* x = static_cast<const T*>(a.x) + row * a.xs;
-    const T* dy = static_cast<const T*>(a.dy) + row * a.ys;
-    const T* in = static_cast<const T*>(a.r) + row * a.rs;
-    const float mean = a.mean[row], rstd = a.rstd[row];
-    Pack<T, V> xw[KB], yw[KB], iw[KB];
-#pragma unroll
-    for (int k = 0; k < KB; ++k) {
-      xw[k] = Pack<T, V>::at(x, at[k].at);
-      yw[k] = Pack<T, V>::at(dy, at[k].at);
-      if constexpr (IN) iw[k] = Pack<T, V>::at(in, at[k].at);
+      for (int k = 0; k < KB; ++k) {
+        x[i][k] = Pack<T, V>::at(x0 + r * xs, at[k].at);
+        y[i][k] = Pack<T, V>::at(y0 + r * ys, at[k].at);
+        if constexpr (IN) in[i][k] = Pack<T, V>::at(in0 + r * rs, at[k].at);
+      }
     }
-    float s1 = 0.f, s2 = 0.f;
+  }
+};
+
+// Columns of a lane: what it adds up
+template <typename T, int V, int KB> struct Columns {
+  float gain[KB][V], dg[KB][V], db[KB][V];
+  Pack<T, V> own[KB];                             // masks: what is another lane's counts as a dy of zero
+  template <int G> __device__ __forceinline__ Columns(const NormArgs& a, const Words<T, V, G, KB>& at) {
+    gains<T, V, G, KB>(a, at, gain);
 #pragma unroll
     for (int k = 0; k < KB; ++k) {
-      float n[V], y[V];
-      xw[k].get(n);
-      (yw[k] & own[k]).get(y);
+      own[k] = Pack<T, V>::from(at[k].skip);
+#pragma unroll
+      for (int j = 0; j < V; ++j) dg[k][j] = db[k][j] = 0.f;
+    }
+  }
+  // this lane's share of the sums of e and of e n over the row
+  __device__ __forceinline__ void add(const Pack<T, V> (&x)[KB], const Pack<T, V> (&y)[KB], unsigned is, float mean, float rstd, float& s1,
+                                      float& s2) {
+    s1 = s2 = 0.f;
+#pragma unroll
+    for (int k = 0; k < KB; ++k) {
+      float n[V], f[V];
+      x[k].get(n);
+      (y[k] & own[k] & is).get(f);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         n[j] = (n[j] - mean) * rstd;
-        dg[k][j] += y[j] * n[j];
-        db[k][j] += y[j];
-        s1 += y[j] * gain[k][j];
-        s2 += y[j] * gain[k][j] * n[j];
+        dg[k][j] += f[j] * n[j];
+        db[k][j] += f[j];
+        f[j] *= gain[k][j];
+        s1 += f[j];
+        s2 += f[j] * n[j];
       }
     }
+  }
+  __device__ __forceinline__ void settle() {
 #pragma unroll
     for (int k = 0; k < KB; ++k)
 #pragma unroll
       for (int j = 0; j < V; ++j) here(dg[k][j]), here(db[k][j]);
+  }
+  // word k of d_x; s1, s2: mean(e), mean(e n)
+  __device__ __forceinline__ void word(int k, const Pack<T, V>& x, const Pack<T, V>& y, float mean, float rstd, float s1, float s2,
+                                       float (&f)[V]) const {
+    float n[V];
+    x.get(n);
+    y.get(f);
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = rstd * (f[j] * gain[k][j] - s1 - (n[j] - mean) * rstd * s2);
+  }
+};
+
+// G <= 64 lanes to a row: no barrier in the loop.  At the end the groups' sums meet in LDS and leave as the workgroup's row of
+// the parts, in the order of the wavefronts.
+template <typename T, int V, int G, int KB, bool IN>
+__global__ __launch_bounds__(kBlock) void norm_bwd_rows_kernel(NormArgs a) {
+  constexpr int kRows = kBlock / G, kWaves = kBlock / 64, kCols = G * KB * V;
+  __shared__ float sh[kWaves][kCols];
+  const int lane = threadIdx.x % G, wave = threadIdx.x >> 6, d = (int)a.d;
+  const float inv = 1.f / (float)d;
+  const Words<T, V, G, KB> at(lane, d);
+  Columns<T, V, KB> c(a, at);
+  int64_t row = row_of<G>((int64_t)blockIdx.x * kRows + threadIdx.x / G);
+  const int64_t step = (int64_t)a.blocks * kRows;
+  Held<T, V, KB, 1, IN> now, next;
+  if (row < a.rows) now.load(a, row, 1, at);
+  for (; row < a.rows; row += step) {
+    next.load(a, row + step < a.rows ? row + step : row, 1, at);
+    float s1, s2;
+    c.add(now.x[0], now.y[0], 0xffffffffu, now.mean[0], now.rstd[0], s1, s2);
+    c.settle();
     s1 = lanes_sum<G>(s1) * inv;
     s2 = lanes_sum<G>(s2) * inv;
     T* out = static_cast<T*>(a.out) + row * a.os;
 #pragma unroll
     for (int k = 0; k < KB; ++k) {
-      float n[V], y[V], f[V];
-      xw[k].renew(s2);
-      yw[k].renew(s2);
-      xw[k].get(n);
-      yw[k].get(y);
-#pragma unroll
-      for (int j = 0; j < V; ++j) f[j] = rstd * (y[j] * gain[k][j] - s1 - (n[j] - mean) * rstd * s2);
+      float f[V];
+      now.x[0][k].renew(s2);
+      now.y[0][k].renew(s2);
+      c.word(k, now.x[0][k], now.y[0][k], now.mean[0], now.rstd[0], s1, s2, f);
       if constexpr (IN) {
-        iw[k].get(n);
+        float g[V];
+        now.in[0][k].get(g);
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] += n[j];
+        for (int j = 0; j < V; ++j) f[j] += g[j];
       }
       if (at[k].skip < V) Pack<T, V>::of(f).to(out, at[k].at);
     }
+    now = next;
   }
   if (!a.parts) return;
-  float* part = a.parts + (int64_t)blockIdx.x * d;
-  auto leave = [&](float (&s)[KB][V], float* to) {
+  auto leave = [&](float (&s)[KB][V], float* part) {
+    if constexpr (G == 16)
 #pragma unroll
-    for (int k = 0; k < KB; ++k)
+      for (int k = 0; k < KB; ++k)
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if constexpr (G == 16) s[k][j] = sum_across_32(sum_across_16(s[k][j]));
+        for (int j = 0; j < V; ++j) s[k][j] = sum_across_32(sum_across_16(s[k][j]));
+    __syncthreads();
+    if ((threadIdx.x & 63) < G)
 #pragma unroll
-    for (int half = kWaves / 2; half > 0; half >>= 1) {
-      __syncthreads();
-      if (wave >= half && wave < 2 * half && (threadIdx.x & 63) < G)
+      for (int k = 0; k < KB; ++k)
 #pragma unroll
-        for (int k = 0; k < KB; ++k)
+        for (int j = 0; j < V; ++j)
+          if (j >= at[k].skip) sh[wave][at[k].at + j] = s[k][j];
+    __syncthreads();
+    for (int i = threadIdx.x; i < d; i += kBlock) {
+      float f = sh[0][i];
 #pragma unroll
-          for (int j = 0; j < V; ++j) sh[wave - half][(k * V + j) * G + lane] = s[k][j];
-      __syncthreads();
-      if (wave < half)
-#pragma unroll
-        for (int k = 0; k < KB; ++k)
-#pragma unroll
-          for (int j = 0; j < V; ++j) s[k][j] += sh[wave][(k * V + j) * G + lane];
+      for (int w = 1; w < kWaves; ++w) f += sh[w][i];
+      part[i] = (a.accumulate ? part[i] : 0.f) + f;
     }
-    if (threadIdx.x >= G) return;
-#pragma unroll
-    for (int k = 0; k < KB; ++k)
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (j >= at[k].skip) to[at[k].at + j] = (a.accumulate ? to[at[k].at + j] : 0.f) + s[k][j];
   };
-  leave(dg, part);
-  leave(db, part + (int64_t)a.blocks * d);
+  float* part = a.parts + (int64_t)blockIdx.x * d;
+  leave(c.dg, part);
+  leave(c.db, part + (int64_t)a.blocks * d);
 }
 
-// ---- backward, a workgroup to a row, R rows at a time: one barrier for the 2 R sums, all of their loads in flight together
-template <typename T, int V, int KB, int R, bool IN>
+// A workgroup to a row, R rows at a time: one barrier for their 2 R sums.  AHEAD: the next rows are requested under the present
+// ones; four words of bf16 to a lane leave no registers for that.
+template <typename T, int V, int KB, int R, bool AHEAD, bool IN>
 __global__ __launch_bounds__(kBlock) void norm_bwd_block_kernel(NormArgs a) {
   __shared__ float sh[2][kBlock / 64][2 * R];
   const int d = (int)a.d;
   const float inv = 1.f / (float)d;
-  float dg[KB][V], db[KB][V], gain[KB][V];
-  Words<T, V, kBlock, KB> at(threadIdx.x, d);
-  gains<T, V, kBlock, KB>(a, at, gain);
-  Pack<T, V> own[KB];
-#pragma unroll
-  for (int k = 0; k < KB; ++k) own[k] = Pack<T, V>::from(at[k].skip);
-#pragma unroll
-  for (int k = 0; k < KB; ++k)
-#pragma unroll
-    for (int j = 0; j < V; ++j) dg[k][j] = db[k][j] = 0.f;
+  const Words<T, V, kBlock, KB> at(threadIdx.x, d);
+  Columns<T, V, KB> c(a, at);
+  int64_t r0 = (int64_t)blockIdx.x * R;
+  const int64_t step = (int64_t)a.blocks * R;
+  auto rows_at = [&](int64_t r) { return (int)min((int64_t)R, a.rows - r); };
+  Held<T, V, KB, R, IN> now, next;
+  if (AHEAD && r0 < a.rows) now.load(a, r0, rows_at(r0), at);
   int turn = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < a.rows; r0 += (int64_t)a.blocks * R, turn ^= 1) {
-    Pack<T, V> xw[R][KB], yw[R][KB], iw[R][KB];
-    float mean[R], rstd[R], s[2 * R];
-    const int there = (int)min((int64_t)R, a.rows - r0);      // rows of this round; the others repeat the last one
-    int64_t xs = a.xs, ys = a.ys, rs = a.rs;
-    asm volatile("" : "+s"(xs), "+s"(ys), "+s"(rs));             // (or every row's address is kept through the loop)
-    const T* x0 = static_cast<const T*>(a.x) + r0 * xs;
-    const T* dy0 = static_cast<const T*>(a.dy) + r0 * ys;
-    const T* in0 = static_cast<const T*>(a.r) + r0 * rs;
+  for (; r0 < a.rows; r0 += step, turn ^= 1) {
+    const int there = rows_at(r0);
+    if constexpr (AHEAD) {
+      const int64_t r1 = r0 + step < a.rows ? r0 + step : r0;
+      next.load(a, r1, rows_at(r1), at);
+    } else {
+      now.load(a, r0, there, at);
+    }
+    float s[2 * R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      const int r = min(i, there - 1);
-      const T *x = x0 + r * xs, *dy = dy0 + r * ys, *in = in0 + r * rs;
-      mean[i] = a.mean[r0 + r];
-      rstd[i] = a.rstd[r0 + r];
+      if (i > 0)                                  // one row's fp32 values at a time
 #pragma unroll
-      for (int k = 0; k < KB; ++k) {
-        xw[i][k] = Pack<T, V>::at(x, at[k].at);
-        yw[i][k] = Pack<T, V>::at(dy, at[k].at);
-        if constexpr (IN) iw[i][k] = Pack<T, V>::at(in, at[k].at);
-      }
+        for (int k = 0; k < KB; ++k) now.x[i][k].renew(s[2 * i - 1]), now.y[i][k].renew(s[2 * i - 1]);
+      c.add(now.x[i], now.y[i], i < there ? 0xffffffffu : 0u, now.mean[i], now.rstd[i], s[2 * i], s[2 * i + 1]);
     }
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const unsigned is = i < there ? 0xffffffffu : 0u;
-      s[2 * i] = s[2 * i + 1] = 0.f;
-#pragma unroll
-      for (int k = 0; k < KB; ++k) {
-        float n[V], y[V];
-        if (i > 0) {                             // one row's fp32 values at a time
-          xw[i][k].renew(s[2 * i - 1]);
-          yw[i][k].renew(s[2 * i - 1]);
-        }
-        xw[i][k].get(n);
-        (yw[i][k] & own[k] & is).get(y);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          n[j] = (n[j] - mean[i]) * rstd[i];
-          dg[k][j] += y[j] * n[j];
-          db[k][j] += y[j];
-          s[2 * i] += y[j] * gain[k][j];
-          s[2 * i + 1] += y[j] * gain[k][j] * n[j];
-        }
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < KB; ++k)
-#pragma unroll
-      for (int j = 0; j < V; ++j) here(dg[k][j]), here(db[k][j]);
-    block_sums<2 * R>(s, sh[turn]);
+    c.settle();
+    block_sums<kBlock, 2 * R>(s, sh[turn]);
     int64_t os = a.os;
     asm volatile("" : "+s"(os));
     T* out0 = static_cast<T*>(a.out) + r0 * os;
-    [[maybe_unused]] float last = s[0];
+    float last = s[0];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const float s1 = s[2 * i] * inv, s2 = s[2 * i + 1] * inv;
-      T* out = out0 + i * os;
 #pragma unroll
       for (int k = 0; k < KB; ++k) {
-        float n[V], y[V], f[V];
-        xw[i][k].renew(s2);
-        yw[i][k].renew(s2);
-        xw[i][k].get(n);
-        yw[i][k].get(y);
-#pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = rstd[i] * (y[j] * gain[k][j] - s1 - (n[j] - mean[i]) * rstd[i] * s2);
+        float f[V];
+        now.x[i][k].renew(last);
+        now.y[i][k].renew(last);
+        c.word(k, now.x[i][k], now.y[i][k], now.mean[i], now.rstd[i], s1, s2, f);
         if constexpr (IN) {
-          iw[i][k].get(n);
+          float g[V];
+          now.in[i][k].get(g);
 #pragma unroll
-          for (int j = 0; j < V; ++j) f[j] += n[j];
+          for (int j = 0; j < V; ++j) f[j] += g[j];
         }
         last = f[V - 1];
-        if (i < there && at[k].skip < V) Pack<T, V>::of(f).to(out, at[k].at);
+        if (i < there && at[k].skip < V) Pack<T, V>::of(f).to(out0 + i * os, at[k].at);
       }
     }
+    if constexpr (AHEAD) now = next;
   }
   if (!a.parts) return;
   float* part = a.parts + (int64_t)blockIdx.x * d;
@@ -436,8 +441,8 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_block_kernel(NormArgs a) {
     for (int j = 0; j < V; ++j)
       if (j >= at[k].skip) {
         float *g = part + at[k].at + j, *b = part_b + at[k].at + j;
-        *g = (a.accumulate ? *g : 0.f) + dg[k][j];
-        *b = (a.accumulate ? *b : 0.f) + db[k][j];
+        *g = (a.accumulate ? *g : 0.f) + c.dg[k][j];
+        *b = (a.accumulate ? *b : 0.f) + c.db[k][j];
       }
 }
 
@@ -471,7 +476,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_long_kernel(NormArgs a) {
       s[0] += e;
       s[1] += e * n;
     }
-    block_sums<2>(s, sh[turn]);
+    block_sums<kBlock, 2>(s, sh[turn]);
     for (int64_t c = threadIdx.x; c < d; c += kBlock) {
       terms(c, n, e, y);
       if (part) {
@@ -520,31 +525,47 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const float* parts, int 
   to[c] = (T)s;
 }
 
-// The kernel for rows of d elements in words of V: f is called with V, the lanes to a row and the words to a lane.
-// 16 lanes up to two words, a wavefront up to four, then a workgroup up to four.
-template <int V, typename F> bool by_length(int64_t d, F f) {
-  using std::integral_constant;
-#define SECO_NORM_CASE(G, KB)                                                                     \
-  if (d <= (G) * (KB) * V) {                                                                       \
-    f(integral_constant<int, V>{}, integral_constant<int, G>{}, integral_constant<int, KB>{});     \
-    return true;                                                                                   \
-  }
-  SECO_NORM_CASE(16, 1)
-  SECO_NORM_CASE(16, 2)
-  SECO_NORM_CASE(64, 1)
-  SECO_NORM_CASE(64, 2)
-  SECO_NORM_CASE(64, 4)
-  SECO_NORM_CASE(kBlock, 1)
-  SECO_NORM_CASE(kBlock, 2)
-  SECO_NORM_CASE(kBlock, 4)
-#undef SECO_NORM_CASE
+// f is called with the elements of a word, the lanes to a row and the words to a lane.
+template <int V, int G, int KB, typename F> bool take(F f) {
+  f(std::integral_constant<int, V>{}, std::integral_constant<int, G>{}, std::integral_constant<int, KB>{});
+  return true;
+}
+
+// Forward, by the words w of a row (16 bytes; rows shorter than that: single elements): 16 lanes up to 32, a wavefront up to 128,
+// then a workgroup, so that no lane has more to load than it keeps in flight at full occupancy.  us for x + residual -> x_out, y:
+//   bf16 2048 elements, a wavefront with four words / 256 lanes with one: 8 rows 4.5 / 3.0, 1024 8.2 / 7.3, 16384 53.8 / 50.7
+//   128 words and few rows, a wavefront / 256 lanes: 128 rows of 1024 bf16 3.8 / 3.3, but 1024 rows 5.5 / 5.9
+//   256 lanes with two words where 512 would be idle by a quarter, once there are rows for every wavefront slot: 16384 rows of 1027
+//   fp32 63 / 54, of 3000 bf16 81 / 74, but 2048 fp32 92 / 99 and 8 rows of 1027 2.8 / 3.0.
+template <typename T, typename F> bool forward_shape(int64_t rows, int64_t d, F f) {
+  constexpr int V = 16 / sizeof(T);
+  if (d < V) return take<1, 16, 1>(f);
+  const int64_t w = (d + V - 1) / V;
+  if (w <= 16) return take<V, 16, 1>(f);
+  if (w <= 32) return take<V, 16, 2>(f);
+  if (w <= 64) return take<V, 64, 1>(f);
+  if (w <= 128 && rows > 512) return take<V, 64, 2>(f);
+  if (w <= 256) return take<V, 256, 1>(f);
+  if (w <= 384 && rows >= 2048) return take<V, 256, 2>(f);
+  if (w <= 512) return take<V, kBlock, 1>(f);
+  if (w <= 1024) return take<V, kBlock, 2>(f);
+  if (w <= 2048) return take<V, kBlock, 4>(f);
   return false;
 }
-// words of 16 bytes, single elements for rows shorter than that
-template <typename T, typename F> bool dispatch(int64_t d, F f) {
+// Backward: a wavefront up to 256 words, whose sums then take half of its registers; a workgroup beyond.
+template <typename T, typename F> bool backward_shape(int64_t d, F f) {
   constexpr int V = 16 / sizeof(T);
-  if (d < V) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{}), true;
-  return by_length<V>(d, f);
+  if (d < V) return take<1, 16, 1>(f);
+  const int64_t w = (d + V - 1) / V;
+  if (w <= 16) return take<V, 16, 1>(f);
+  if (w <= 32) return take<V, 16, 2>(f);
+  if (w <= 64) return take<V, 64, 1>(f);
+  if (w <= 128) return take<V, 64, 2>(f);
+  if (w <= 256) return take<V, 64, 4>(f);
+  if (w <= 512) return take<V, kBlock, 1>(f);
+  if (w <= 1024) return take<V, kBlock, 2>(f);
+  if (w <= 2048) return take<V, kBlock, 4>(f);
+  return false;
 }
 
 dim3 rows_grid(int64_t workgroups) {
@@ -552,8 +573,8 @@ dim3 rows_grid(int64_t workgroups) {
 }
 
 template <typename T> int norm_fwd(const NormArgs& a, hipStream_t s) {
-  const bool done = dispatch<T>(a.d, [&](auto v, auto g, auto kb) {
-    constexpr int G = decltype(g)::value, kRows = G > 256 ? 1 : 256 / G;
+  const bool done = forward_shape<T>(a.rows, a.d, [&](auto v, auto g, auto kb) {
+    constexpr int G = decltype(g)::value, kRows = G >= 256 ? 1 : 256 / G;
     hipLaunchKernelGGL((norm_fwd_kernel<T, decltype(v)::value, G, decltype(kb)::value>), rows_grid((a.rows + kRows - 1) / kRows),
                        dim3(G > 256 ? G : 256), 0, s, a);
   });
@@ -561,22 +582,23 @@ template <typename T> int norm_fwd(const NormArgs& a, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? SECO_OK : SECO_ERR_LAUNCH;
 }
 
-constexpr int rows_at_once(int kb) { return kb == 4 ? 2 : 4; }
+template <typename T> constexpr bool ahead(int kb) { return kb < 4 || sizeof(T) == 4; }
+template <typename T> constexpr int rows_at_once(int kb) { return ahead<T>(kb) ? 4 / kb : 2; }
 template <typename T> int rows_of_block(int64_t d) {      // rows that a workgroup of the backward takes at a time
   int n = 1;
-  dispatch<T>(d, [&](auto, auto g, auto kb) {
+  backward_shape<T>(d, [&](auto, auto g, auto kb) {
     constexpr int G = decltype(g)::value;
-    n = G <= 64 ? kBlock / G : rows_at_once(decltype(kb)::value);
+    n = G <= 64 ? kBlock / G : rows_at_once<T>(decltype(kb)::value);
   });
   return n;
 }
 
 template <typename T> int norm_bwd(const NormArgs& a, hipStream_t s) {
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.blocks), dim3(kBlock), 0, s, a); };
-  const bool done = dispatch<T>(a.d, [&](auto v, auto g, auto kb) {
+  const bool done = backward_shape<T>(a.d, [&](auto v, auto g, auto kb) {
     constexpr int V = decltype(v)::value, G = decltype(g)::value, KB = decltype(kb)::value;
     if constexpr (G <= 64) a.r ? launch(norm_bwd_rows_kernel<T, V, G, KB, true>) : launch(norm_bwd_rows_kernel<T, V, G, KB, false>);
-    else a.r ? launch(norm_bwd_block_kernel<T, V, KB, rows_at_once(KB), true>) : launch(norm_bwd_block_kernel<T, V, KB, rows_at_once(KB), false>);
+    else a.r ? launch(norm_bwd_block_kernel<T, V, KB, rows_at_once<T>(KB), ahead<T>(KB), true>) : launch(norm_bwd_block_kernel<T, V, KB, rows_at_once<T>(KB), ahead<T>(KB), false>);
   });
   if (!done) hipLaunchKernelGGL(norm_bwd_long_kernel<T>, dim3(a.blocks), dim3(kBlock), 0, s, a);
   return hipGetLastError() == hipSuccess ? SECO_OK : SECO_ERR_LAUNCH;
