@@ -328,6 +328,47 @@ int layer_norm_bwd(const layer_norm_desc* desc, const void* x, const void* gain,
 size_t layer_norm_workspace_bytes(const layer_norm_desc* desc);
 
 /*
+ * The AdamW update of many tensors (decoupled weight decay), the step behind a training step's gradients.  With t = steps
+ * taken before + 1 and g = grad_scale * gradient, element by element, in fp32 (the factors of t in fp64):
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+ *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * Tensors are flat: n elements each, one behind the other; any alignment of their elements.  Launches take up to 48 tensors
+ * of one kind (types, master) each.
+ *   tensors_host  HOST array of n_tensors entries, read before the call returns.  No two tensors may overlap.  n = 0: skipped
+ *   param         in/out; master (fp32, bf16 parameters only, or NULL): what is updated instead, the parameter is its rounding
+ *   m, v          state_bits 32: fp32 [n].  state_bits 8: e4m3 codes [n] of m and of sqrt(v), in units of m_scale, v_scale:
+ *                 one fp32 per 256 consecutive elements of the tensor (the last block may be short), the block's largest finite
+ *                 magnitude / 448 (at least 2^-126).  A sqrt(v) > 0 is stored as at least the smallest code, 2^-9.  The update
+ *                 uses m and v before they are rounded.  All zeros (codes and scales) is the state before the first step.
+ *   step          device, two int64: [0] steps taken so far, read and incremented by the call (so that a captured graph
+ *                 counts on when it is replayed); [1] the call's own, 0 before and after every call
+ *   lr_device, grad_scale_device   device fp32, or NULL: read when the kernels run; lr_device replaces lr
+ * A gradient that is not finite makes its element of p NaN, and of the states what that element alone would be.
+ * Errors: SECO_ERR_RANGE for lr, eps, weight_decay not finite or negative and betas outside [0, 1); SECO_ERR_DTYPE for
+ * state_bits or a dtype that is none, and for a master of an fp32 parameter.
+ */
+typedef struct adamw_tensor {
+  void* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;           /* state_bits 8 only */
+  float* v_scale;
+  float* master;
+  int64_t n;
+  int32_t param_dtype;      /* seco_dtype */
+  int32_t grad_dtype;
+  float weight_decay;
+} adamw_tensor;
+typedef struct adamw_desc {
+  double lr, beta1, beta2, eps;
+  const float* lr_device;
+  const float* grad_scale_device;
+  int32_t state_bits;       /* 32 or 8, for all tensors of the call */
+} adamw_desc;
+int adamw_step(const adamw_desc* desc, const adamw_tensor* tensors_host, int32_t n_tensors, int64_t* step, void* hip_stream);
+
+/*
  * SpaCO chunk selection (Alg. 2, selection step: t different chunks out of k, uniformly), host only.
  * Deterministic in (seed, step): SplitMix64 stream keyed by (seed, step), unbiased bounded
  * draws by rejection, first t steps of a Fisher-Yates shuffle of 0..k-1, result sorted in

@@ -7,6 +7,7 @@ PyTorch fallback: if the library has not been built, importing the binding raise
 """
 from .binding import (  # noqa: F401
     SecoError,
+    adamw_step,
     kv_append,
     kvgrad_accumulate,
     kvgrad_readout,

@@ -250,6 +250,19 @@ def layer_norm_bwd(x, gain, mean, rstd, d_y, d_in=None, d_x=None, with_gain=True
     return (_ext or _load_ext()).norm_bwd(x, gain, mean, rstd, d_y, d_in, d_x, with_gain, with_bias, ws, stream)
 
 
+def adamw_step(params, grads, m, v, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, masters=None, m_scales=None,
+               v_scales=None, grad_scale=None, stream=None):
+    """One AdamW step of many tensors, in place (lists of tensors, one entry per parameter).
+
+    params, grads: bf16 or fp32; grads, m, v and masters have their parameter's shape and strides, and a parameter lies dense
+    in memory.  m, v: fp32, or float8_e4m3fn beside m_scales, v_scales (fp32, one per 256 elements), where v holds sqrt(v).
+    masters: fp32 tensors or None, of bf16 parameters.  step: int64 [steps taken, 0] on the GPU, counted on by the call.
+    lr: a float, or a one-element fp32 tensor on the GPU; grad_scale: likewise a tensor, or None; weight_decay: a float or
+    one per parameter."""
+    (_ext or _load_ext()).adamw(params, grads, m, v, step, lr, betas[0], betas[1], eps, weight_decay, masters, m_scales, v_scales,
+                                grad_scale, stream)
+
+
 def spaco_select_chunks(seed, step, k, t):
     """t distinct chunk indices of 0..k-1, descending (list of int)."""
     out = (C.c_int32 * max(int(t), 1))()

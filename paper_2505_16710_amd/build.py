@@ -36,6 +36,7 @@ SOURCES = [
     "gemm_bf16.hip",
     "train_ops_api.cpp",
     "layer_norm.hip",
+    "adamw.hip",
 ]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

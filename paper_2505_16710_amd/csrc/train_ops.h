@@ -34,4 +34,29 @@ int launch_norm_bwd(const NormArgs& a, hipStream_t s);
 // d_gain, d_bias (either NULL) = parts added up over the blocks in their order
 int launch_norm_sums(const float* parts, int blocks, int64_t d, void* d_gain, void* d_bias, int gain_f32, hipStream_t s);
 
+// ---- AdamW.  What a launch needs of a tensor, and of its tensors together; passed by value.
+constexpr int kAdamTensors = 48;               // of a launch: its arguments stay below 4 KiB
+constexpr int64_t kAdamSpan = 4096;            // elements that a workgroup takes at a time
+struct AdamEntry {
+  void* p;
+  const void* g;
+  void *m, *v;
+  float *m_scale, *v_scale, *master;
+  uint32_t first, last;                        // its spans among the launch's
+  int tail;                                    // elements of the last one
+  float decay;
+};
+struct AdamArgs {
+  AdamEntry e[kAdamTensors];
+  double lr, beta1, beta2;
+  float eps;
+  const float *lr_at, *grad_scale;             // or NULL
+  int64_t* step;
+  uint32_t spans;
+  int count, last;                             // last: the launch that counts the step
+};
+// kind: bits 0 param bf16, 1 gradient bf16, 2 master, 3 states of 8 bits
+enum { kAdamParamBf16 = 1, kAdamGradBf16 = 2, kAdamMaster = 4, kAdam8 = 8 };
+int launch_adamw(int kind, const AdamArgs& a, hipStream_t s);
+
 }  // namespace seco

@@ -39,6 +39,27 @@ NormArgs norm_args(const layer_norm_desc* d) {
 }
 bool rows_apart(const layer_norm_desc* d, int64_t stride) { return d->rows < 2 || stride >= d->d; }
 
+// ---- AdamW
+bool fraction(double b) { return b >= 0.0 && b < 1.0; }
+int check_adamw(const adamw_desc* d, const adamw_tensor& t) {
+  if (t.n < 0) return SECO_ERR_SHAPE;
+  if (!std::isfinite(t.weight_decay) || t.weight_decay < 0.f) return SECO_ERR_RANGE;
+  if (!is_dtype(t.param_dtype) || !is_dtype(t.grad_dtype) || (t.master && t.param_dtype != SECO_BF16)) return SECO_ERR_DTYPE;
+  if (t.n > (int64_t)1 << 40) return SECO_ERR_TOO_LARGE;
+  if (t.n == 0) return SECO_OK;
+  const bool eight = d->state_bits == 8;
+  if (!t.param || !t.grad || !t.m || !t.v || (eight && (!t.m_scale || !t.v_scale))) return SECO_ERR_NULL;
+  const int state = eight ? 1 : 4;
+  if (!aligned(t.param, elem(t.param_dtype)) || !aligned(t.grad, elem(t.grad_dtype)) || !aligned(t.m, state) || !aligned(t.v, state) ||
+      !aligned(t.master, 4) || (eight && (!aligned(t.m_scale, 4) || !aligned(t.v_scale, 4))))
+    return SECO_ERR_ALIGN;
+  return SECO_OK;
+}
+int kind_of(const adamw_desc* d, const adamw_tensor& t) {
+  return (t.param_dtype == SECO_BF16 ? kAdamParamBf16 : 0) | (t.grad_dtype == SECO_BF16 ? kAdamGradBf16 : 0) | (t.master ? kAdamMaster : 0) |
+         (d->state_bits == 8 ? kAdam8 : 0);
+}
+
 }  // namespace
 }  // namespace seco
 
@@ -100,4 +121,45 @@ extern "C" int layer_norm_bwd(const layer_norm_desc* desc, const void* x, const 
   rc = launch_norm_bwd(a, s);
   if (rc || !sums) return rc;
   return launch_norm_sums(a.parts, a.blocks, a.d, d_gain, d_bias, a.gain_f32, s);
+}
+
+extern "C" int adamw_step(const adamw_desc* desc, const adamw_tensor* tensors_host, int32_t n_tensors, int64_t* step, void* hip_stream) {
+  if (!desc || !step || (n_tensors > 0 && !tensors_host)) return SECO_ERR_NULL;
+  if (n_tensors < 0) return SECO_ERR_SHAPE;
+  if (desc->state_bits != 8 && desc->state_bits != 32) return SECO_ERR_DTYPE;
+  if (!std::isfinite(desc->lr) || desc->lr < 0.0 || !fraction(desc->beta1) || !fraction(desc->beta2) || !std::isfinite(desc->eps) ||
+      desc->eps < 0.0)
+    return SECO_ERR_RANGE;
+  if (!aligned(step, 8) || !aligned(desc->lr_device, 4) || !aligned(desc->grad_scale_device, 4)) return SECO_ERR_ALIGN;
+  for (int32_t i = 0; i < n_tensors; ++i)
+    if (const int rc = check_adamw(desc, tensors_host[i])) return rc;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  AdamArgs a{};
+  a.lr = desc->lr;
+  a.beta1 = desc->beta1;
+  a.beta2 = desc->beta2;
+  a.eps = (float)desc->eps;
+  a.lr_at = desc->lr_device;
+  a.grad_scale = desc->grad_scale_device;
+  a.step = step;
+  // Tensors of one kind share launches; one that is full waits for the next tensor, so that the last launch is known as such.
+  int pending = 0, rc = SECO_OK;
+  for (int kind = 0; kind < 16 && !rc; ++kind)
+    for (int32_t i = 0; i < n_tensors && !rc; ++i) {
+      const adamw_tensor& t = tensors_host[i];
+      if (t.n == 0 || kind_of(desc, t) != kind) continue;
+      const uint32_t spans = (uint32_t)((t.n + kAdamSpan - 1) / kAdamSpan);     // below 2^29
+      if (a.count == kAdamTensors || (a.count && (pending != kind || a.spans + spans > (uint32_t)1 << 30))) {
+        rc = launch_adamw(pending, a, s);
+        a.count = 0;
+        a.spans = 0;
+      }
+      pending = kind;
+      a.e[a.count++] = AdamEntry{t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.master, a.spans, a.spans + spans - 1,
+                                 (int)(t.n - (int64_t)(spans - 1) * kAdamSpan), t.weight_decay};
+      a.spans += spans;
+    }
+  if (rc) return rc;
+  a.last = 1;
+  return launch_adamw(pending, a, s);
 }

@@ -1,4 +1,7 @@
 // Binding of the operators around the training step (train_ops_api.cpp).  Third source of the extension module.
+#include <algorithm>
+#include <memory>
+
 #include <c10/core/DeviceGuard.h>
 
 #include "binding_common.h"
@@ -155,8 +158,118 @@ PyObject* norm_bwd(PyObject* const* a) {
   return Py_BuildValue("NNN", out_ref(a[6], dx), wrap(dg), wrap(db));
 }
 
+// ---- AdamW
+struct Sequence {                                // of tensors, or none
+  PyObject* s;
+  Py_ssize_t n;
+  explicit Sequence(PyObject* o) : s(nullptr), n(0) {
+    if (o == Py_None) return;
+    s = PySequence_Fast(o, "expected a sequence of tensors");
+    if (!s) throw Raised{};
+    n = PySequence_Fast_GET_SIZE(s);
+  }
+  ~Sequence() { Py_XDECREF(s); }
+  Sequence(const Sequence&) = delete;
+  PyObject* item(Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(s, i); }
+  const Tensor& operator[](Py_ssize_t i) const { return tensor(item(i)); }
+};
+[[noreturn]] void bad(PyObject* type, const char* what, Py_ssize_t i, const char* expected) {
+  PyErr_Format(type, "%s[%zd]: %s", what, i, expected);
+  throw Raised{};
+}
+// laid out like the parameter: the same elements at the same places
+void same_places(const Tensor& t, const Tensor& p, const char* what, Py_ssize_t i) {
+  bool same = t.sizes() == p.sizes();
+  for (int64_t k = 0; same && k < p.dim(); ++k) same = p.size(k) < 2 || t.stride(k) == p.stride(k);
+  if (!same) bad(PyExc_ValueError, what, i, "must have the shape and strides of its parameter");
+  if (t.device() != p.device()) bad(PyExc_ValueError, what, i, "must be on its parameter's device");
+}
+const float* scalar_on(const Tensor& t, const Tensor& like_t, const char* what) {
+  if (t.scalar_type() != at::kFloat || t.numel() != 1 || t.device() != like_t.device()) {
+    PyErr_Format(PyExc_ValueError, "%s: a float, or a float32 tensor of one element on the parameters' device", what);
+    throw Raised{};
+  }
+  return fptr(t);
+}
+
+// (params, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, masters, m_scales, v_scales, grad_scale, stream)
+PyObject* adamw(PyObject* const* a) {
+  const Sequence params(a[0]), grads(a[1]), ms(a[2]), vs(a[3]), masters(a[10]),
+      m_scales(a[11]), v_scales(a[12]);
+  const Tensor& step = tensor(a[4]);
+  const Py_ssize_t n = params.n;
+  if (grads.n != n || ms.n != n || vs.n != n || (masters.s && masters.n != n)) raise(PyExc_ValueError, "one gradient, m, v (and master) per parameter");
+  if ((m_scales.s == nullptr) != (v_scales.s == nullptr) || (m_scales.s && (m_scales.n != n || v_scales.n != n)))
+    raise(PyExc_ValueError, "states of 8 bits: one m_scale and one v_scale per parameter; states of 32: neither");
+  if (step.scalar_type() != at::kLong || step.numel() != 2 || !step.is_contiguous())
+    raise(PyExc_ValueError, "step: a contiguous int64 tensor of two elements, steps taken and 0");
+  const bool eight = m_scales.s != nullptr, decays = !PyFloat_Check(a[9]) && !PyLong_Check(a[9]);
+  std::vector<float> decay;
+  if (decays) decay = floats(a[9]);
+  if (decays && (Py_ssize_t)decay.size() != n) raise(PyExc_ValueError, "weight_decay: one value, or one per parameter");
+  const float one_decay = decays ? 0.f : (float)real(a[9]);
+  adamw_desc d{};
+  if (THPVariable_Check(a[5])) d.lr_device = scalar_on(tensor(a[5]), step, "lr");
+  else d.lr = real(a[5]);
+  if (a[13] != Py_None) d.grad_scale_device = scalar_on(tensor(a[13]), step, "grad_scale");
+  d.beta1 = real(a[6]);
+  d.beta2 = real(a[7]);
+  d.eps = real(a[8]);
+  d.state_bits = eight ? 8 : 32;
+  const auto list = std::make_unique<adamw_tensor[]>((size_t)n);
+  std::vector<std::pair<uintptr_t, uintptr_t>> places;
+  places.reserve((size_t)n);
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    const Tensor &p = params[i], &g = grads[i], &m = ms[i], &v = vs[i];
+    adamw_tensor& t = list[i];
+    if ((p.scalar_type() != at::kFloat && p.scalar_type() != at::kBFloat16) || (g.scalar_type() != at::kFloat && g.scalar_type() != at::kBFloat16))
+      bad(PyExc_TypeError, "params", i, "parameter and gradient must be bfloat16 or float32");
+    if (!p.is_non_overlapping_and_dense()) bad(PyExc_ValueError, "params", i, "must lie dense in memory, in any order of its dimensions");
+    if (p.device() != step.device()) bad(PyExc_ValueError, "params", i, "must be on the device of step");
+    const at::ScalarType state = eight ? at::kFloat8_e4m3fn : at::kFloat;
+    if (m.scalar_type() != state || v.scalar_type() != state)
+      bad(PyExc_TypeError, "m, v", i, eight ? "must be float8_e4m3fn beside scales" : "must be float32 without scales");
+    same_places(g, p, "grads", i);
+    same_places(m, p, "m", i);
+    same_places(v, p, "v", i);
+    t.n = p.numel();
+    t.param = ptr(p);
+    t.grad = ptr(g);
+    t.m = ptr(m);
+    t.v = ptr(v);
+    t.param_dtype = dtype_code(p);
+    t.grad_dtype = dtype_code(g);
+    t.weight_decay = decays ? decay[(size_t)i] : one_decay;
+    t.m_scale = t.v_scale = t.master = nullptr;
+    if (eight) {
+      for (const Tensor* x : {&m_scales[i], &v_scales[i]})
+        if (x->scalar_type() != at::kFloat || !x->is_contiguous() || x->numel() != (t.n + 255) / 256 || x->device() != p.device())
+          bad(PyExc_ValueError, "m_scales, v_scales", i, "one contiguous float32 per 256 elements of the parameter");
+      t.m_scale = fptr(m_scales[i]);
+      t.v_scale = fptr(v_scales[i]);
+    }
+    if (masters.s && masters.item(i) != Py_None) {
+      const Tensor& w = masters[i];
+      if (w.scalar_type() != at::kFloat || p.scalar_type() != at::kBFloat16) bad(PyExc_TypeError, "masters", i, "float32, of bfloat16 parameters only");
+      same_places(w, p, "masters", i);
+      t.master = fptr(w);
+    }
+    if (t.n > 0) places.emplace_back((uintptr_t)t.param, (uintptr_t)t.param + nbytes(p));
+  }
+  std::sort(places.begin(), places.end());
+  for (size_t i = 1; i < places.size(); ++i)
+    if (places[i].first < places[i - 1].second) raise(PyExc_ValueError, "params: two of them overlap, or one is there twice");
+  if (!step.is_cuda()) raise(PyExc_ValueError, "the tensors must be on one GPU");
+  OnGpu on(step, a[14]);
+  check(lib.adamw_step(&d, list.get(), (int32_t)n, static_cast<int64_t*>(ptr(step)), on.s), "adamw_step");
+  // (what autograd has kept of a parameter's old values is out of date now)
+  for (Py_ssize_t i = 0; i < n; ++i)
+    if (!params[i].is_inference()) params[i].unsafeGetTensorImpl()->bump_version();
+  Py_RETURN_NONE;
+}
+
 }  // namespace
 
-PyMethodDef train_methods[] = {SECO_METHOD("norm_fwd", norm_fwd, 8), SECO_METHOD("norm_bwd", norm_bwd, 11), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef train_methods[] = {SECO_METHOD("adamw", adamw, 15), SECO_METHOD("norm_fwd", norm_fwd, 8), SECO_METHOD("norm_bwd", norm_bwd, 11), {nullptr, nullptr, 0, nullptr}};
 
 }  // namespace seco_ext

@@ -238,6 +238,29 @@ def test_layouts(d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t,d", [("bf16", 5), ("bf16", 100), ("bf16", 250), ("bf16", 1027), ("bf16", 2048), ("bf16", 4100), ("bf16", 8200),
+                                 ("bf16", 20001), ("f32", 1027), ("f32", 4096), ("f32", 8000)])
+@pytest.mark.parametrize("rows", [1, 2, 5, 31, 1030])
+def test_what_lies_behind_the_rows_stays(t, d, rows):
+    dtype = TYPES[t]
+    rows = min(rows, max(2, (1 << 21) // d))
+    x, r, dy = (_rows(90 + i, rows, d, dtype).to(DEV) for i in range(3))
+    gain = torch.ones(d, dtype=dtype, device=DEV)
+
+    def room():
+        return torch.full((rows + 8, d + 3), 77.0, dtype=dtype, device=DEV)
+    bufs = [room() for _ in range(3)]
+    y, out, dx = (b[4:4 + rows, 1:1 + d] for b in bufs)
+    _, mean, rstd, _ = seco.layer_norm_fwd(x, gain, residual=r, y=y, x_out=out)
+    seco.layer_norm_bwd(out, gain, mean, rstd, dy, d_in=r, d_x=dx)
+    seco.layer_norm_bwd(out, gain, mean, rstd, dy, d_x=dx)
+    for b in bufs:
+        assert (b[4:4 + rows, 1:1 + d] != 77).any()
+        b[4:4 + rows, 1:1 + d] = 77
+        assert (b == 77).all()
+
+
+@pytest.mark.gpu
 def test_more_rows_than_a_grid_holds_along_x():
     """16 short rows to a workgroup, 2^22 workgroups along x: the rows behind them."""
     rows = (1 << 26) + 5
