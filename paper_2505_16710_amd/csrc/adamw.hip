@@ -21,7 +21,7 @@
 namespace seco {
 namespace {
 
-constexpr int kThreads = 256, kBlockLen = 256, kUnroll = (int)(kAdamSpan / kThreads / 4);
+constexpr int kThreads = 256, kBlockLen = 256;
 constexpr float kTop = 448.f, kLeast = 0x1p-9f;      // the largest and the smallest positive e4m3 value
 
 // b^t for t >= 1
@@ -88,14 +88,14 @@ template <typename P, typename G, bool MASTER, int BITS> struct Lane {
 
 // n: elements of the block; FULL: all 256
 template <bool FULL, typename T> __device__ __forceinline__ Pack<T, 4> read(const T* p, unsigned c, int n) {
-  if constexpr (FULL) return Pack<T, 4>::at(p, c);
+  if constexpr (FULL) return Pack<T, 4>::once(p, c);
   float f[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) f[j] = (int)c + j < n ? (float)p[c + j] : 0.f;
   return Pack<T, 4>::of(f);
 }
 template <bool FULL, typename T> __device__ __forceinline__ void write(T* p, unsigned c, int n, const float (&f)[4]) {
-  if constexpr (FULL) return Pack<T, 4>::of(f).to(p, c);
+  if constexpr (FULL) return Pack<T, 4>::of(f).away(p, c);
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     if ((int)c + j < n) p[c + j] = (T)f[j];
@@ -104,7 +104,8 @@ template <bool FULL> __device__ __forceinline__ unsigned read_codes(const void* 
   const uint8_t* p = static_cast<const uint8_t*>(at);
   unsigned u = 0;
   if constexpr (FULL) {
-    __builtin_memcpy(&u, p + c, 4);
+    typedef unsigned loose __attribute__((aligned(1)));
+    u = __builtin_nontemporal_load(reinterpret_cast<const loose*>(p + c));
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -115,7 +116,8 @@ template <bool FULL> __device__ __forceinline__ unsigned read_codes(const void* 
 template <bool FULL> __device__ __forceinline__ void write_codes(void* at, unsigned c, int n, unsigned u) {
   uint8_t* p = static_cast<uint8_t*>(at);
   if constexpr (FULL) {
-    __builtin_memcpy(p + c, &u, 4);
+    typedef unsigned loose __attribute__((aligned(1)));
+    __builtin_nontemporal_store(u, reinterpret_cast<loose*>(p + c));
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -186,14 +188,15 @@ __device__ __forceinline__ void update(const Lane<P, G, MASTER, BITS>& l, const 
 
 template <typename P, typename G, bool MASTER, int BITS>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamArgs a) {
+  constexpr int kSpan = (int)adam_span(BITS == 8), kUnroll = kSpan / kThreads / 4;
   __shared__ Factors shared;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // The step's number is read by one wavefront of a workgroup, which then draws a number of its own; whoever draws the last one
-  // knows that all have read it, and counts the step.
+  // The step's number is read by one wavefront of a workgroup.  Where it has not been counted, that one then draws a number of
+  // its own; whoever draws the last one knows that all have read it, and counts the step.
   unsigned drawn = 0;
   int64_t t = 0;
   if (wave == 0) {
-    t = a.step[0] + 1;
+    t = a.step[0] + (a.counted ? 0 : 1);
     if (a.last && lane == 0) {
       unsigned one = 1;
       asm volatile("" : "+v"(one) : "v"((unsigned)t));         // (behind the read)
@@ -211,12 +214,12 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamArgs a) {
   for (unsigned span = blockIdx.x; span < a.spans; span += gridDim.x) {
     const int i = __builtin_popcountll(__builtin_amdgcn_ballot_w64(first <= span)) - 1;
     const AdamEntry& e = a.e[i];
-    const int64_t at0 = (int64_t)(span - e.first) * kAdamSpan;
+    const int64_t at0 = (int64_t)(span - e.first) * kSpan;
     // (32 bits: of a 64-bit comparison of scalars this compiler has taken the minimum by a flag that was overwritten before)
-    const int left = span == e.last ? e.tail : (int)kAdamSpan;
+    const int left = span == e.last ? e.tail : kSpan;
     const float keep = 1.f - k.lr * e.decay;
     Lane<P, G, MASTER, BITS> l[kUnroll];
-    if (left == (int)kAdamSpan) {
+    if (left == kSpan) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) fetch<P, G, MASTER, BITS, true>(l[u], e, at0 + (u * 4 + wave) * kBlockLen, lane * 4, 0);
 #pragma unroll
@@ -242,6 +245,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamArgs a) {
   }
 }
 
+__global__ void adamw_count_kernel(int64_t* step) { step[0] += 1; }
+
 template <typename P, typename G, bool MASTER> void launch(bool eight, const AdamArgs& a, unsigned grid, hipStream_t s) {
   if (eight) hipLaunchKernelGGL((adamw_kernel<P, G, MASTER, 8>), dim3(grid), dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL((adamw_kernel<P, G, MASTER, 32>), dim3(grid), dim3(kThreads), 0, s, a);
@@ -249,10 +254,14 @@ template <typename P, typename G, bool MASTER> void launch(bool eight, const Ada
 
 }  // namespace
 
-int device_cus();                              // (seco_api.hip)
+int launch_adamw_count(int64_t* step, hipStream_t s) {
+  hipLaunchKernelGGL(adamw_count_kernel, dim3(1), dim3(1), 0, s, step);
+  return hipGetLastError() == hipSuccess ? SECO_OK : SECO_ERR_LAUNCH;
+}
 
 int launch_adamw(int kind, const AdamArgs& a, hipStream_t s) {
-  const unsigned most = 8u * (unsigned)device_cus(), grid = a.spans < 1 ? 1 : a.spans < most ? a.spans : most;
+  constexpr unsigned kMost = 1u << 22;           // (a launch holds fewer than 2^32 threads in a dimension)
+  const unsigned grid = a.spans < 1 ? 1 : a.spans < kMost ? a.spans : kMost;
   const bool eight = kind & kAdam8;
   switch (kind & ~kAdam8) {
     case 0: launch<float, float, false>(eight, a, grid, s); break;

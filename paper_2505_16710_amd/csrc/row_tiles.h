@@ -24,6 +24,38 @@ template <typename T, int V> struct Pack {
     }
     return x;
   }
+  // the same for what is not used again: marked so that it does not push other data out of the caches
+  __device__ __forceinline__ static Pack once(const T* p) {
+    if constexpr (sizeof(T) * V >= 4) {
+      typedef unsigned words __attribute__((ext_vector_type(kWords)));
+      typedef words loose __attribute__((aligned(sizeof(T))));
+      const words u = __builtin_nontemporal_load(reinterpret_cast<const loose*>(p));
+      Pack x;
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) x.w[i] = u[i];
+      return x;
+    } else {
+      return at(p);
+    }
+  }
+  __device__ __forceinline__ void away(T* p) const {
+    if constexpr (sizeof(T) * V >= 4) {
+      typedef unsigned words __attribute__((ext_vector_type(kWords)));
+      typedef words loose __attribute__((aligned(sizeof(T))));
+      words u;
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) u[i] = w[i];
+      __builtin_nontemporal_store(u, reinterpret_cast<loose*>(p));
+    } else {
+      to(p);
+    }
+  }
+  __device__ __forceinline__ static Pack once(const T* row, unsigned c) {
+    return once(reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + c * (unsigned)sizeof(T)));
+  }
+  __device__ __forceinline__ void away(T* row, unsigned c) const {
+    away(reinterpret_cast<T*>(reinterpret_cast<char*>(row) + c * (unsigned)sizeof(T)));
+  }
   // element c of a row (rows are shorter than 2^32 bytes: a scalar base and a 32-bit offset)
   __device__ __forceinline__ static Pack at(const T* row, unsigned c) {
     return at(reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + c * (unsigned)sizeof(T)));

@@ -36,7 +36,11 @@ int launch_norm_sums(const float* parts, int blocks, int64_t d, void* d_gain, vo
 
 // ---- AdamW.  What a launch needs of a tensor, and of its tensors together; passed by value.
 constexpr int kAdamTensors = 48;               // of a launch: its arguments stay below 4 KiB
-constexpr int64_t kAdamSpan = 4096;            // elements that a workgroup takes at a time
+// Elements of a workgroup: two blocks of 256 to a wavefront, one where states of 8 bits take the wavefront's reductions
+constexpr int64_t adam_span(bool eight) { return eight ? 1024 : 2048; }
+// Up to so many workgroups count the step themselves, each by an addition to one place; of more, these additions (11 ns each, one
+// behind the other) take longer than a launch in front that counts it (2 us)
+constexpr uint32_t kAdamCounting = 128;
 struct AdamEntry {
   void* p;
   const void* g;
@@ -53,10 +57,12 @@ struct AdamArgs {
   const float *lr_at, *grad_scale;             // or NULL
   int64_t* step;
   uint32_t spans;
-  int count, last;                             // last: the launch that counts the step
+  int count;
+  int counted, last;                           // counted: the step is already; else `last` is the launch that counts it
 };
 // kind: bits 0 param bf16, 1 gradient bf16, 2 master, 3 states of 8 bits
 enum { kAdamParamBf16 = 1, kAdamGradBf16 = 2, kAdamMaster = 4, kAdam8 = 8 };
 int launch_adamw(int kind, const AdamArgs& a, hipStream_t s);
+int launch_adamw_count(int64_t* step, hipStream_t s);
 
 }  // namespace seco

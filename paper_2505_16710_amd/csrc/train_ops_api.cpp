@@ -133,7 +133,6 @@ extern "C" int adamw_step(const adamw_desc* desc, const adamw_tensor* tensors_ho
   if (!aligned(step, 8) || !aligned(desc->lr_device, 4) || !aligned(desc->grad_scale_device, 4)) return SECO_ERR_ALIGN;
   for (int32_t i = 0; i < n_tensors; ++i)
     if (const int rc = check_adamw(desc, tensors_host[i])) return rc;
-  hipStream_t s = static_cast<hipStream_t>(hip_stream);
   AdamArgs a{};
   a.lr = desc->lr;
   a.beta1 = desc->beta1;
@@ -142,24 +141,32 @@ extern "C" int adamw_step(const adamw_desc* desc, const adamw_tensor* tensors_ho
   a.lr_at = desc->lr_device;
   a.grad_scale = desc->grad_scale_device;
   a.step = step;
+  hipStream_t hs = static_cast<hipStream_t>(hip_stream);
+  const int64_t span = adam_span(desc->state_bits == 8);
+  int64_t all = 0;
+  for (int32_t i = 0; i < n_tensors; ++i) all += (tensors_host[i].n + span - 1) / span;
+  if (all > kAdamCounting) {
+    if (const int rc = launch_adamw_count(step, hs)) return rc;
+    a.counted = 1;
+  }
   // Tensors of one kind share launches; one that is full waits for the next tensor, so that the last launch is known as such.
   int pending = 0, rc = SECO_OK;
   for (int kind = 0; kind < 16 && !rc; ++kind)
     for (int32_t i = 0; i < n_tensors && !rc; ++i) {
       const adamw_tensor& t = tensors_host[i];
       if (t.n == 0 || kind_of(desc, t) != kind) continue;
-      const uint32_t spans = (uint32_t)((t.n + kAdamSpan - 1) / kAdamSpan);     // below 2^29
-      if (a.count == kAdamTensors || (a.count && (pending != kind || a.spans + spans > (uint32_t)1 << 30))) {
-        rc = launch_adamw(pending, a, s);
+      const uint32_t spans = (uint32_t)((t.n + span - 1) / span);      // at most 2^30
+      if (a.count == kAdamTensors || (a.count && (pending != kind || a.spans + spans > (uint32_t)1 << 31))) {
+        rc = launch_adamw(pending, a, hs);
         a.count = 0;
         a.spans = 0;
       }
       pending = kind;
       a.e[a.count++] = AdamEntry{t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.master, a.spans, a.spans + spans - 1,
-                                 (int)(t.n - (int64_t)(spans - 1) * kAdamSpan), t.weight_decay};
+                                 (int)(t.n - (int64_t)(spans - 1) * span), t.weight_decay};
       a.spans += spans;
     }
-  if (rc) return rc;
-  a.last = 1;
-  return launch_adamw(pending, a, s);
+  if (rc || (a.counted && !a.count)) return rc;
+  a.last = !a.counted;
+  return launch_adamw(pending, a, hs);
 }
