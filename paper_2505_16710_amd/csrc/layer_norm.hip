@@ -79,8 +79,18 @@ template <int TH, int N> __device__ __forceinline__ void block_sums(float (&x)[N
   for (int i = 0; i < N; ++i) x[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i));
 }
 
+// Words of the rows.  FAR: of tensors that no cache holds until they are used again (see far_apart): past the caches.
+template <bool FAR, typename T, int V> __device__ __forceinline__ Pack<T, V> word_at(const T* row, unsigned c) {
+  if constexpr (FAR) return Pack<T, V>::once(row, c);
+  else return Pack<T, V>::at(row, c);
+}
+template <bool FAR, typename T, int V> __device__ __forceinline__ void word_to(const Pack<T, V>& w, T* row, unsigned c) {
+  if constexpr (FAR) w.away(row, c);
+  else w.to(row, c);
+}
+
 // ---- forward: G lanes to a row, KB words of V elements to a lane
-template <typename T, int V, int G, int KB>
+template <typename T, int V, int G, int KB, bool FAR>
 __global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_kernel(NormArgs a) {
   constexpr int kRows = G >= 256 ? 1 : 256 / G;
   __shared__ float sh[2][G / 64 + 1][2];
@@ -100,10 +110,10 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_kernel(NormArgs a)
   }
   Pack<T, V> w[KB], rw[KB];
 #pragma unroll
-  for (int k = 0; k < KB; ++k) w[k] = Pack<T, V>::at(x, Place<V, G>(k, lane, d).at);
+  for (int k = 0; k < KB; ++k) w[k] = word_at<FAR, T, V>(x, Place<V, G>(k, lane, d).at);
   if (r)
 #pragma unroll
-    for (int k = 0; k < KB; ++k) rw[k] = Pack<T, V>::at(r, Place<V, G>(k, lane, d).at);
+    for (int k = 0; k < KB; ++k) rw[k] = word_at<FAR, T, V>(r, Place<V, G>(k, lane, d).at);
   float f[KB][V], sum[1] = {0.f};
 #pragma unroll
   for (int k = 0; k < KB; ++k) {
@@ -170,8 +180,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_kernel(NormArgs a)
 #pragma unroll
       for (int j = 0; j < V; ++j) g[j] += b[j];
     }
-    if (out) w[k].to(out, p.at);
-    Pack<T, V>::of(g).to(y, p.at);
+    if (out) word_to<FAR>(w[k], out, p.at);
+    word_to<FAR>(Pack<T, V>::of(g), y, p.at);
   }
 }
 
@@ -234,7 +244,7 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_long_kernel(NormArgs a) {
 // ---- backward.  A workgroup keeps the gain and the sums of its lanes' columns in registers and takes rows in turn, the next
 // ones requested before the present ones are worked on: with one workgroup to a CU nothing else covers the arithmetic.
 // What a group of lanes holds of R rows: words of x, dy and d_in, and the rows' statistics
-template <typename T, int V, int KB, int R, bool IN> struct Held {
+template <typename T, int V, int KB, int R, bool IN, bool FAR> struct Held {
   Pack<T, V> x[R][KB], y[R][KB], in[IN ? R : 1][IN ? KB : 1];
   float mean[R], rstd[R];
   // rows r0 .. r0 + there - 1; of the others the last one again
@@ -251,9 +261,9 @@ template <typename T, int V, int KB, int R, bool IN> struct Held {
       rstd[i] = a.rstd[r0 + r];
 #pragma unroll
       for (int k = 0; k < KB; ++k) {
-        x[i][k] = Pack<T, V>::at(x0 + r * xs, at[k].at);
-        y[i][k] = Pack<T, V>::at(y0 + r * ys, at[k].at);
-        if constexpr (IN) in[i][k] = Pack<T, V>::at(in0 + r * rs, at[k].at);
+        x[i][k] = word_at<FAR, T, V>(x0 + r * xs, at[k].at);
+        y[i][k] = word_at<FAR, T, V>(y0 + r * ys, at[k].at);
+        if constexpr (IN) in[i][k] = word_at<FAR, T, V>(in0 + r * rs, at[k].at);
       }
     }
   }
@@ -321,7 +331,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_rows_kernel(NormArgs a) {
   Columns<T, V, KB> c(a, at);
   int64_t row = row_of<G>((int64_t)blockIdx.x * kRows + threadIdx.x / G);
   const int64_t step = (int64_t)a.blocks * kRows;
-  Held<T, V, KB, 1, IN> now, next;
+  Held<T, V, KB, 1, IN, false> now, next;
   if (row < a.rows) now.load(a, row, 1, at);
   for (; row < a.rows; row += step) {
     next.load(a, row + step < a.rows ? row + step : row, 1, at);
@@ -376,7 +386,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_rows_kernel(NormArgs a) {
 
 // A workgroup to a row, R rows at a time: one barrier for their 2 R sums.  AHEAD: the next rows are requested under the present
 // ones; four words of bf16 to a lane leave no registers for that.
-template <typename T, int V, int KB, int R, bool AHEAD, bool IN>
+template <typename T, int V, int KB, int R, bool AHEAD, bool IN, bool FAR>
 __global__ __launch_bounds__(kBlock) void norm_bwd_block_kernel(NormArgs a) {
   __shared__ float sh[2][kBlock / 64][2 * R];
   const int d = (int)a.d;
@@ -386,7 +396,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_block_kernel(NormArgs a) {
   int64_t r0 = (int64_t)blockIdx.x * R;
   const int64_t step = (int64_t)a.blocks * R;
   auto rows_at = [&](int64_t r) { return (int)min((int64_t)R, a.rows - r); };
-  Held<T, V, KB, R, IN> now, next;
+  Held<T, V, KB, R, IN, FAR> now, next;
   if (AHEAD && r0 < a.rows) now.load(a, r0, rows_at(r0), at);
   int turn = 0;
   for (; r0 < a.rows; r0 += step, turn ^= 1) {
@@ -427,7 +437,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_block_kernel(NormArgs a) {
           for (int j = 0; j < V; ++j) f[j] += g[j];
         }
         last = f[V - 1];
-        if (i < there && at[k].skip < V) Pack<T, V>::of(f).to(out0 + i * os, at[k].at);
+        if (i < there && at[k].skip < V) word_to<FAR>(Pack<T, V>::of(f), out0 + i * os, at[k].at);
       }
     }
     if constexpr (AHEAD) now = next;
@@ -568,6 +578,17 @@ template <typename T, typename F> bool backward_shape(int64_t d, F f) {
   return false;
 }
 
+// Whether a call's results are more than the 256 MiB of the last cache, so that nothing of them is there when they are read:
+// its words then go past the caches.  Only for whole 16-byte words at their places: the others share lines with their
+// neighbours.  us with / without: backward 16384 x 8192 bf16 150 / 164; but a second norm behind one of 8192 x 4096 93 / 84.
+bool far_apart(const NormArgs& a, int elem, int results) {
+  const int64_t per = 16 / elem;
+  for (int64_t n : {a.d, a.xs, a.rs, a.os, a.ys})
+    if (n % per) return false;
+  for (const void* p : {a.x, a.r, (const void*)a.out, a.dy, (const void*)a.y})
+    if (reinterpret_cast<uintptr_t>(p) & 15u) return false;
+  return a.rows * a.d * elem * results >= (int64_t)1 << 28;
+}
 dim3 rows_grid(int64_t workgroups) {
   return dim3((unsigned)(workgroups < kGridX ? workgroups : kGridX), (unsigned)((workgroups + kGridX - 1) / kGridX));
 }
@@ -575,8 +596,10 @@ dim3 rows_grid(int64_t workgroups) {
 template <typename T> int norm_fwd(const NormArgs& a, hipStream_t s) {
   const bool done = forward_shape<T>(a.rows, a.d, [&](auto v, auto g, auto kb) {
     constexpr int G = decltype(g)::value, kRows = G >= 256 ? 1 : 256 / G;
-    hipLaunchKernelGGL((norm_fwd_kernel<T, decltype(v)::value, G, decltype(kb)::value>), rows_grid((a.rows + kRows - 1) / kRows),
-                       dim3(G > 256 ? G : 256), 0, s, a);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, rows_grid((a.rows + kRows - 1) / kRows), dim3(G > 256 ? G : 256), 0, s, a); };
+    if constexpr (G >= 256)
+      if (far_apart(a, sizeof(T), a.out ? 2 : 1)) return launch(norm_fwd_kernel<T, decltype(v)::value, G, decltype(kb)::value, true>);
+    launch(norm_fwd_kernel<T, decltype(v)::value, G, decltype(kb)::value, false>);
   });
   if (!done) hipLaunchKernelGGL(norm_fwd_long_kernel<T>, rows_grid(a.rows), dim3(kBlock), 0, s, a);
   return hipGetLastError() == hipSuccess ? SECO_OK : SECO_ERR_LAUNCH;
@@ -598,7 +621,12 @@ template <typename T> int norm_bwd(const NormArgs& a, hipStream_t s) {
   const bool done = backward_shape<T>(a.d, [&](auto v, auto g, auto kb) {
     constexpr int V = decltype(v)::value, G = decltype(g)::value, KB = decltype(kb)::value;
     if constexpr (G <= 64) a.r ? launch(norm_bwd_rows_kernel<T, V, G, KB, true>) : launch(norm_bwd_rows_kernel<T, V, G, KB, false>);
-    else a.r ? launch(norm_bwd_block_kernel<T, V, KB, rows_at_once<T>(KB), ahead<T>(KB), true>) : launch(norm_bwd_block_kernel<T, V, KB, rows_at_once<T>(KB), ahead<T>(KB), false>);
+    else {
+      constexpr int R = rows_at_once<T>(KB);
+      constexpr bool kAhead = ahead<T>(KB);
+      if (far_apart(a, sizeof(T), 1)) a.r ? launch(norm_bwd_block_kernel<T, V, KB, R, kAhead, true, true>) : launch(norm_bwd_block_kernel<T, V, KB, R, kAhead, false, true>);
+      else a.r ? launch(norm_bwd_block_kernel<T, V, KB, R, kAhead, true, false>) : launch(norm_bwd_block_kernel<T, V, KB, R, kAhead, false, false>);
+    }
   });
   if (!done) hipLaunchKernelGGL(norm_bwd_long_kernel<T>, dim3(a.blocks), dim3(kBlock), 0, s, a);
   return hipGetLastError() == hipSuccess ? SECO_OK : SECO_ERR_LAUNCH;

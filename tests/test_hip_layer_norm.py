@@ -261,6 +261,34 @@ def test_what_lies_behind_the_rows_stays(t, d, rows):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t,d", [("bf16", 2048), ("bf16", 8192), ("bf16", 16384), ("f32", 4096)])
+def test_results_that_no_cache_holds(t, d):
+    """256 MiB and more of them take other accesses: every row is what it is in a call of a few rows."""
+    dtype = TYPES[t]
+    rows = (1 << 28) // (d * torch.finfo(dtype).bits // 8) + 3
+    g = torch.Generator(device=DEV).manual_seed(d)
+    x, r, dy = (torch.randn(rows, d, generator=g, device=DEV, dtype=dtype) for _ in range(3))
+    gain = torch.ones(d, dtype=dtype, device=DEV)
+    y, mean, rstd, out = seco.layer_norm_fwd(x, gain, residual=r)
+    dx, dg, db = seco.layer_norm_bwd(out, gain, mean, rstd, dy, d_in=r)
+    dx2 = seco.layer_norm_bwd(out, gain, mean, rstd, dy, with_gain=False, with_bias=False)[0]
+    for at in (slice(0, 600), slice(rows // 2, rows // 2 + 600), slice(rows - 600, rows)):
+        few = seco.layer_norm_fwd(x[at], gain, residual=r[at])
+        assert all(torch.equal(a[at], b) for a, b in zip((y, mean, rstd, out), few))
+        assert torch.equal(dx[at], seco.layer_norm_bwd(out[at], gain, mean[at], rstd[at], dy[at], d_in=r[at])[0])
+        assert torch.equal(dx2[at], seco.layer_norm_bwd(out[at], gain, mean[at], rstd[at], dy[at])[0])
+    ref, size = torch.zeros(2, d, dtype=torch.float64, device=DEV), torch.zeros(2, d, dtype=torch.float64, device=DEV)
+    for at in range(0, rows, 4096):
+        y64 = dy[at:at + 4096].double()
+        n = (out[at:at + 4096].double() - mean[at:at + 4096, None].double()) * rstd[at:at + 4096, None].double()
+        ref += torch.stack([(y64 * n).sum(0), y64.sum(0)])
+        size += torch.stack([(y64 * n).abs().sum(0), y64.abs().sum(0)])
+    # a share's chain is up to rows / 256 long, 64 U for 40 terms above
+    bound = 64 * U * max(1, rows / 256 / 40) * size + _half(dtype) * ref.abs()
+    assert ((torch.stack([dg, db]).double() - ref).abs() <= bound).all()
+
+
+@pytest.mark.gpu
 def test_more_rows_than_a_grid_holds_along_x():
     """16 short rows to a workgroup, 2^22 workgroups along x: the rows behind them."""
     rows = (1 << 26) + 5
