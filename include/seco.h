@@ -293,6 +293,48 @@ int rope_rotate(const seco_desc* desc, int32_t n_heads, const void* x_in, void* 
                 float rope_base, int32_t inverse, void* hip_stream);
 
 /*
+ * Rotary positions with several axes, for sequences that hold images or video beside text: every row has a position on each of
+ * up to SECO_ROPE_MAX_AXES axes (time, height, width), and every pair (x[i], x[i + D/2]), i < D/2, of a row belongs to one
+ * axis: it turns by position[axis of i] * frequency(i).
+ *   sections         pairs of each axis; they add up to D/2
+ *   interleaved      0: the first sections[0] pairs belong to axis 0, the next sections[1] to axis 1, ...
+ *                    1: pairs are dealt to the axes in turn; an axis that has its number is passed over
+ *   own_frequencies  0: frequency(i) = base^(-2 i / D), one ladder over all pairs (rows whose positions are equal on all
+ *                    axes then turn as rope_rotate turns them, to rounding)
+ *                    1: each axis has a ladder of its own: base^(-k / sections[axis]) for its k-th pair
+ * positions   DEVICE int64, the position of row r of batch b on axis x at positions[x * s[0] + b * s[1] + r * s[2]],
+ *             pos_stride = s (HOST, elements, not negative; s[1] = 0: one sequence of positions for all batches).  Any
+ *             value of magnitude below 2^40, negative ones too.  Row r is the call's own row (0 .. chunk_len).
+ * Angles, sines, cosines and products are fp64; the result is rounded once.  head_dim: a multiple of 8 up to 256, bf16 and fp32
+ * alike; batch, head_dim, chunk_len and dtype of desc are used, and:
+ *   rope_rotate_axes   x_out = R(+-theta) x_in for [B, n_heads, C, D] tensors, q_stride (in) and o_stride (out); x_out may be
+ *                      x_in (equal strides)
+ *   rope_append_axes   a layer's way from its projections to the attention in one launch: queries [B, n_q_heads, C, D]
+ *                      (q_stride) turned to q_out (o_stride; may be q), keys and values [B, n_kv_heads, C, D] (g_stride, in
+ *                      elements of dtype) turned / copied to rows q_start + r of the caches (kv_stride)
+ *   rope_readout_axes  and the gradients' way back: d_q (q_stride) turned back to d_q_out (o_stride; may be d_q),
+ *                      d_k_new = R(-theta)(scaler * gk[rows]), d_v_new = scaler * gv[rows] for rows q_start + r of gk, gv (fp32,
+ *                      g_stride), d_k_new and d_v_new with kv_stride
+ * A pair of pointers (q and q_out, k_new and k_cache, ...) may be NULL (skipped).
+ */
+#define SECO_ROPE_MAX_AXES 4
+typedef struct rope_axes {
+  int32_t n_axes;
+  int32_t interleaved;
+  int32_t own_frequencies;
+  float base;                             /* finite, > 1 (SECO_ERR_RANGE, as for sections that do not add up) */
+  int32_t sections[SECO_ROPE_MAX_AXES];
+} rope_axes;
+int rope_rotate_axes(const seco_desc* desc, const rope_axes* axes, int32_t n_heads, const void* x_in, void* x_out,
+                     const int64_t* positions, const int64_t* pos_stride, int32_t inverse, void* hip_stream);
+int rope_append_axes(const seco_desc* desc, const rope_axes* axes, const void* q, void* q_out, const void* k_new,
+                     const void* v_new, void* k_cache, void* v_cache, const int64_t* positions, const int64_t* pos_stride,
+                     void* hip_stream);
+int rope_readout_axes(const seco_desc* desc, const rope_axes* axes, const void* d_q, void* d_q_out, const float* gk,
+                      const float* gv, void* d_k_new, void* d_v_new, float scaler, const int64_t* positions,
+                      const int64_t* pos_stride, void* hip_stream);
+
+/*
  * Layer norm of rows, with an optional residual add in front, and its backward (operators of the models that the chunk calls
  * are used in; not part of the paper).  Rows have d elements, d of any size, contiguous; the strides between rows are given.
  * Pointers need the alignment of their elements only.  Statistics, sums and products are fp32; a result is rounded once.

@@ -6,6 +6,7 @@ include/seco.h.  Every step of the path runs in the HIP kernels; PyTorch is used
 PyTorch fallback: if the library has not been built, importing the binding raises.
 """
 from .binding import (  # noqa: F401
+    RopeAxes,
     SecoError,
     adamw_step,
     kv_append,
@@ -16,7 +17,10 @@ from .binding import (  # noqa: F401
     layer_norm_fwd,
     library_path,
     load_library,
+    rope_append_axes,
+    rope_readout_axes,
     rope_rotate,
+    rope_rotate_axes,
     seco_chunk_attn_bwd,
     seco_chunk_attn_bwd_gather,
     seco_chunk_attn_bwd_noalloc,

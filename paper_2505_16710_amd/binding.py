@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 # SECO_LIBRARY overrides the path (e.g. to try a library built with other tile parameters)
@@ -233,6 +234,43 @@ def kvgrad_readout(gk, gv, row_begin, n_rows, dtype, scaler=1.0, d_k=None, d_v=N
 def rope_rotate(x, pos_start, rope_base, inverse=False, out=None, stream=None):
     """Rotary position embedding of x [B, H, C, D] (row r at position pos_start + r), or its inverse / transpose."""
     return (_ext or _load_ext()).rotate(x, pos_start, rope_base, inverse, out, stream)
+
+
+class RopeAxes:
+    """Rotary positions with several axes: which pairs of a head turn with which axis, and by what frequency.
+
+    sections: pairs of each axis, one to four of them, adding up to head_dim / 2.  interleaved: pairs are dealt to the axes in
+    turn (else in one run per axis).  own_frequencies: a ladder base^(-k / n) over each axis' n pairs (else one,
+    base^(-2 i / head_dim), over all).  Built once and kept by the program."""
+
+    def __init__(self, sections, base, interleaved=False, own_frequencies=False):
+        self.sections = tuple(int(n) for n in sections)
+        self.base, self.interleaved, self.own_frequencies = float(base), bool(interleaved), bool(own_frequencies)
+        if not 1 <= len(self.sections) <= 4 or min(self.sections) < 0 or not 4 <= sum(self.sections) <= 128 or sum(self.sections) % 4:
+            raise ValueError("sections: one to four numbers of pairs that add up to a multiple of 4, at most 128")
+        if not 1.0 < self.base < float("inf"):
+            raise ValueError("base must be finite and above 1")
+        self.head_dim = 2 * sum(self.sections)
+        self.packed = struct.pack("=3if4i", len(self.sections), self.interleaved, self.own_frequencies, self.base,
+                                  *(self.sections + (0, 0, 0))[:4])
+
+
+def rope_rotate_axes(x, positions, axes, inverse=False, out=None, stream=None):
+    """x [B, H, C, D] turned by its rows' positions on the axes (RopeAxes), or back.  positions: int64 [axes, B or 1, C] on the
+    GPU, any strides.  out may be x."""
+    return (_ext or _load_ext()).rotate_axes(x, positions, axes.packed, inverse, out, stream)
+
+
+def rope_append_axes(q, k_new, v_new, k_cache, v_cache, row_begin, positions, axes, q_out=None, stream=None):
+    """One launch from the projections to the attention: queries [B, Hq, C, D] (or None) turned, returned; keys [B, Hkv, C, D]
+    turned and values copied to cache rows [row_begin, row_begin + C).  q_out may be q."""
+    return (_ext or _load_ext()).append_axes(q, k_new, v_new, k_cache, v_cache, row_begin, positions, axes.packed, q_out, stream)
+
+
+def rope_readout_axes(d_q, gk, gv, row_begin, positions, axes, scaler=1.0, dq_out=None, d_k=None, d_v=None, dtype=None, stream=None):
+    """The gradients' way back, one launch: (d_q turned back or None, d_k, d_v) with d_k, d_v = scaler * (gk turned back, gv)
+    for buffer rows [row_begin, row_begin + C), C the positions' rows, in d_q's dtype (without d_q: dtype).  dq_out may be d_q."""
+    return (_ext or _load_ext()).readout_axes(d_q, gk, gv, row_begin, positions, axes.packed, scaler, dq_out, d_k, d_v, dtype, stream)
 
 
 def layer_norm_fwd(x, gain=None, bias=None, eps=1e-5, residual=None, y=None, x_out=None, stream=None):

@@ -37,6 +37,7 @@ SOURCES = [
     "train_ops_api.cpp",
     "layer_norm.hip",
     "adamw.hip",
+    "rope_axes.hip",
 ]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -65,4 +65,24 @@ enum { kAdamParamBf16 = 1, kAdamGradBf16 = 2, kAdamMaster = 4, kAdam8 = 8 };
 int launch_adamw(int kind, const AdamArgs& a, hipStream_t s);
 int launch_adamw_count(int64_t* step, hipStream_t s);
 
+// ---- rotary positions with several axes.  A tensor pair of a call: rows in and rows out, head heads of each batch.
+constexpr int kRopeMaxPairs = 128;
+struct RopePart {
+  const void* in;
+  void* out;
+  int64_t is[3], os[3];                        // (batch, head, row) strides in elements
+  int heads;
+};
+struct RopeAxesArgs {
+  double frequency[kRopeMaxPairs];
+  uint8_t axis[kRopeMaxPairs];
+  RopePart q, k, v;                            // q, k: turned; v: as it is (heads 0: not there)
+  const int64_t* positions;
+  int64_t ps[3];                               // (axis, batch, row) strides
+  int B, C, D, n_axes;
+  float scale;                                 // of k and v
+};
+// bf16: the type of q and of what k and v give; wide_in: k and v are fp32 all the same
+int launch_rope_axes(const RopeAxesArgs& a, bool bf16, bool wide_in, bool inverse, hipStream_t s);   // wide_in: inverse only
+
 }  // namespace seco

@@ -60,10 +60,122 @@ int kind_of(const adamw_desc* d, const adamw_tensor& t) {
          (d->state_bits == 8 ? kAdam8 : 0);
 }
 
+// ---- rotary positions with several axes
+int check_rope_axes(const seco_desc* d, const rope_axes* x, const int64_t* positions, const int64_t* pos_stride) {
+  if (!d || !x || !positions || !pos_stride) return SECO_ERR_NULL;
+  if (!is_dtype(d->dtype)) return SECO_ERR_DTYPE;
+  if (d->batch < 1 || d->chunk_len < 1 || d->head_dim < 1 || d->q_start < 0) return SECO_ERR_SHAPE;
+  if (d->head_dim % 8 != 0 || d->head_dim > 2 * kRopeMaxPairs) return SECO_ERR_HEAD_DIM;
+  if (d->batch > 65535 || d->chunk_len > 1 << 27 || (int64_t)d->q_start + d->chunk_len > (int64_t)1 << 30) return SECO_ERR_TOO_LARGE;
+  if (x->n_axes < 1 || x->n_axes > SECO_ROPE_MAX_AXES || !std::isfinite(x->base) || !(x->base > 1.f)) return SECO_ERR_RANGE;
+  int64_t sum = 0;
+  for (int i = 0; i < x->n_axes; ++i) {
+    if (x->sections[i] < 0) return SECO_ERR_RANGE;
+    sum += x->sections[i];
+  }
+  if (sum != d->head_dim / 2) return SECO_ERR_RANGE;
+  if (!aligned(positions, 8)) return SECO_ERR_ALIGN;
+  for (int i = 0; i < 3; ++i) {
+    if (pos_stride[i] < 0) return SECO_ERR_SHAPE;
+    if (pos_stride[i] > (int64_t)1 << 40) return SECO_ERR_TOO_LARGE;
+  }
+  return SECO_OK;
+}
+// frequencies and axes of the pairs, positions
+void fill_rope(RopeAxesArgs& a, const seco_desc* d, const rope_axes* x, const int64_t* positions, const int64_t* pos_stride) {
+  const int pairs = d->head_dim / 2;
+  int left[SECO_ROPE_MAX_AXES], seen[SECO_ROPE_MAX_AXES] = {};
+  for (int i = 0; i < x->n_axes; ++i) left[i] = x->sections[i];
+  for (int i = 0, axis = 0; i < pairs; ++i) {
+    while (left[axis] == 0) axis = axis + 1 == x->n_axes ? 0 : axis + 1;   // (some axis lacks pairs: they add up)
+    a.axis[i] = (uint8_t)axis;
+    const double of = x->own_frequencies ? (double)seen[axis] / x->sections[axis] : (double)i / pairs;
+    a.frequency[i] = std::exp2(-of * std::log2((double)x->base));
+    ++seen[axis];
+    --left[axis];
+    if (x->interleaved) axis = axis + 1 == x->n_axes ? 0 : axis + 1;
+  }
+  a.positions = positions;
+  for (int i = 0; i < 3; ++i) a.ps[i] = pos_stride[i];
+  a.B = d->batch;
+  a.C = d->chunk_len;
+  a.D = d->head_dim;
+  a.n_axes = x->n_axes;
+  a.scale = 1.f;
+}
+// one tensor pair; rows from in_row, out_row on.  Rows start on 16-byte boundaries, as everywhere.
+int set_part(RopePart& p, const seco_desc* d, const void* in, void* out, int heads, const int64_t* is, const int64_t* os, int in_elem,
+             int out_elem, int64_t in_row, int64_t out_row) {
+  if ((in == nullptr) != (out == nullptr)) return SECO_ERR_NULL;
+  if (!in) return SECO_OK;
+  if (heads < 1) return SECO_ERR_SHAPE;
+  if (heads > 65535) return SECO_ERR_TOO_LARGE;
+  for (int i = 0; i < 3; ++i) {
+    if (is[i] < 0 || is[i] * in_elem % 16 || os[i] < 0 || os[i] * out_elem % 16) return SECO_ERR_ALIGN;
+    if (is[i] > (int64_t)1 << 40 || os[i] > (int64_t)1 << 40) return SECO_ERR_TOO_LARGE;
+  }
+  if (is[2] < d->head_dim || os[2] < d->head_dim) return SECO_ERR_ALIGN;
+  if (!aligned(in, 16) || !aligned(out, 16)) return SECO_ERR_ALIGN;
+  p.in = static_cast<const char*>(in) + in_row * is[2] * in_elem;
+  p.out = static_cast<char*>(out) + out_row * os[2] * out_elem;
+  for (int i = 0; i < 3; ++i) {
+    p.is[i] = is[i];
+    p.os[i] = os[i];
+  }
+  p.heads = heads;
+  return SECO_OK;
+}
+
 }  // namespace
 }  // namespace seco
 
 using namespace seco;
+
+extern "C" int rope_rotate_axes(const seco_desc* desc, const rope_axes* axes, int32_t n_heads, const void* x_in, void* x_out,
+                                const int64_t* positions, const int64_t* pos_stride, int32_t inverse, void* hip_stream) {
+  int rc = check_rope_axes(desc, axes, positions, pos_stride);
+  if (rc) return rc;
+  if (!x_in || !x_out) return SECO_ERR_NULL;
+  RopeAxesArgs a{};
+  const int e = elem(desc->dtype);
+  if ((rc = set_part(a.q, desc, x_in, x_out, n_heads, desc->q_stride, desc->o_stride, e, e, 0, 0))) return rc;
+  fill_rope(a, desc, axes, positions, pos_stride);
+  return launch_rope_axes(a, desc->dtype == SECO_BF16, false, inverse != 0, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int rope_append_axes(const seco_desc* desc, const rope_axes* axes, const void* q, void* q_out, const void* k_new,
+                                const void* v_new, void* k_cache, void* v_cache, const int64_t* positions, const int64_t* pos_stride,
+                                void* hip_stream) {
+  int rc = check_rope_axes(desc, axes, positions, pos_stride);
+  if (rc) return rc;
+  RopeAxesArgs a{};
+  const int e = elem(desc->dtype);
+  const int64_t row = desc->q_start;
+  if ((rc = set_part(a.q, desc, q, q_out, desc->n_q_heads, desc->q_stride, desc->o_stride, e, e, 0, 0))) return rc;
+  if ((rc = set_part(a.k, desc, k_new, k_cache, desc->n_kv_heads, desc->g_stride, desc->kv_stride, e, e, 0, row))) return rc;
+  if ((rc = set_part(a.v, desc, v_new, v_cache, desc->n_kv_heads, desc->g_stride, desc->kv_stride, e, e, 0, row))) return rc;
+  if (!q && !k_new && !v_new) return SECO_OK;
+  fill_rope(a, desc, axes, positions, pos_stride);
+  return launch_rope_axes(a, desc->dtype == SECO_BF16, false, false, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int rope_readout_axes(const seco_desc* desc, const rope_axes* axes, const void* d_q, void* d_q_out, const float* gk,
+                                 const float* gv, void* d_k_new, void* d_v_new, float scaler, const int64_t* positions,
+                                 const int64_t* pos_stride, void* hip_stream) {
+  int rc = check_rope_axes(desc, axes, positions, pos_stride);
+  if (rc) return rc;
+  if (!std::isfinite(scaler)) return SECO_ERR_RANGE;
+  RopeAxesArgs a{};
+  const int e = elem(desc->dtype);
+  const int64_t row = desc->q_start;
+  if ((rc = set_part(a.q, desc, d_q, d_q_out, desc->n_q_heads, desc->q_stride, desc->o_stride, e, e, 0, 0))) return rc;
+  if ((rc = set_part(a.k, desc, gk, d_k_new, desc->n_kv_heads, desc->g_stride, desc->kv_stride, 4, e, row, 0))) return rc;
+  if ((rc = set_part(a.v, desc, gv, d_v_new, desc->n_kv_heads, desc->g_stride, desc->kv_stride, 4, e, row, 0))) return rc;
+  if (!d_q && !gk && !gv) return SECO_OK;
+  fill_rope(a, desc, axes, positions, pos_stride);
+  a.scale = scaler;
+  return launch_rope_axes(a, desc->dtype == SECO_BF16, desc->dtype == SECO_BF16, true, static_cast<hipStream_t>(hip_stream));
+}
 
 extern "C" size_t layer_norm_workspace_bytes(const layer_norm_desc* desc) {
   if (check_norm(desc)) return (size_t)-1;

@@ -1,5 +1,6 @@
 // Binding of the operators around the training step (train_ops_api.cpp).  Third source of the extension module.
 #include <algorithm>
+#include <cstring>
 #include <memory>
 
 #include <c10/core/DeviceGuard.h>
@@ -268,8 +269,225 @@ PyObject* adamw(PyObject* const* a) {
   Py_RETURN_NONE;
 }
 
+// ---- rotary positions with several axes
+struct Axes {
+  rope_axes x;
+  int64_t head_dim = 0;
+  explicit Axes(PyObject* o) {
+    char* p;
+    Py_ssize_t n;
+    if (PyBytes_AsStringAndSize(o, &p, &n) < 0) throw Raised{};
+    if (n != (Py_ssize_t)sizeof(x)) raise(PyExc_TypeError, "axes: expected a RopeAxes");
+    memcpy(&x, p, sizeof(x));
+    for (int i = 0; i < x.n_axes && i < SECO_ROPE_MAX_AXES; ++i) head_dim += 2 * (int64_t)x.sections[i];
+  }
+};
+// int64 [axes, B or 1, rows]; strides in elements
+void positions_of(const Tensor& t, const Axes& axes, int64_t B, int64_t rows, int64_t out[3]) {
+  if (t.scalar_type() != at::kLong || t.dim() != 3 || t.size(0) != axes.x.n_axes || (t.size(1) != B && t.size(1) != 1) || t.size(2) != rows) {
+    PyErr_Format(PyExc_ValueError, "positions: expected int64 [%d, %lld or 1, %lld]", (int)axes.x.n_axes, (long long)B, (long long)rows);
+    throw Raised{};
+  }
+  for (int i = 0; i < 3; ++i) out[i] = t.size(i) == 1 ? 0 : t.stride(i);
+}
+void heads_tensor(const Tensor& t, const char* name, int64_t B, int64_t rows, int64_t D, at::ScalarType type) {
+  if (t.dim() == 4 && t.size(0) == B && t.size(2) == rows && t.size(3) == D && t.stride(3) == 1 && t.scalar_type() == type) return;
+  PyErr_Format(PyExc_ValueError, "%s: expected a [%lld, heads, %lld, %lld] tensor of the call's dtype with contiguous head_dim", name,
+               (long long)B, (long long)rows, (long long)D);
+  throw Raised{};
+}
+// k / v or their like: one shape, one set of strides
+void like_each_other(const Tensor& a, const Tensor& b, const char* names) {
+  if (a.sizes() == b.sizes() && a.strides() == b.strides() && a.scalar_type() == b.scalar_type()) return;
+  PyErr_Format(PyExc_ValueError, "%s must share shape, strides and dtype", names);
+  throw Raised{};
+}
+// rows [begin, begin + n) of a cache or gradient buffer [B, H, N, D]
+void rows_inside(const Tensor& t, const char* name, int64_t B, int64_t H, int64_t D, int64_t begin, int64_t n, at::ScalarType type) {
+  if (t.dim() == 4 && t.size(0) == B && t.size(1) == H && t.size(3) == D && t.stride(3) == 1 && t.scalar_type() == type && begin >= 0 &&
+      begin + n <= t.size(2))
+    return;
+  PyErr_Format(PyExc_ValueError, "%s: expected [%lld, %lld, rows, %lld] with contiguous head_dim that holds rows %lld to %lld", name,
+               (long long)B, (long long)H, (long long)D, (long long)begin, (long long)(begin + n));
+  throw Raised{};
+}
+// what is written: every element at a place of its own
+void writable(const Tensor& t, const char* name) {
+  for (int64_t i = 0; i < t.dim(); ++i)
+    if (t.size(i) > 1 && t.stride(i) == 0) {
+      PyErr_Format(PyExc_ValueError, "%s: an expanded tensor cannot be written", name);
+      throw Raised{};
+    }
+}
+// a dimension of one element may have any stride; the library asks for one that keeps rows on their boundaries
+void heads_strides(const Tensor& t, int64_t out[3]) {
+  for (int i = 0; i < 3; ++i) out[i] = t.size(i) == 1 ? (i == 2 ? t.size(3) : 0) : t.stride(i);
+}
+seco_desc axes_desc(int64_t B, int64_t rows, int64_t D, at::ScalarType type, int64_t row_begin, const char* where) {
+  if (B > 65535 || rows > 1 << 27 || D > 256 || row_begin > (int64_t)1 << 30) check(SECO_ERR_TOO_LARGE, where);
+  seco_desc d{};
+  d.q_start = (int32_t)row_begin;
+  d.batch = (int32_t)B;
+  d.n_q_heads = d.n_kv_heads = 1;
+  d.chunk_len = (int32_t)rows;
+  d.head_dim = (int32_t)D;
+  d.dtype = type == at::kBFloat16 ? SECO_BF16 : SECO_F32;
+  d.softmax_scale = 1.f;
+  return d;
+}
+void fits_axes(const Axes& axes, int64_t D) {
+  if (axes.head_dim == D) return;
+  PyErr_Format(PyExc_ValueError, "axes: their sections make a head_dim of %lld, not %lld", (long long)axes.head_dim, (long long)D);
+  throw Raised{};
+}
+
+// (x, positions, axes, inverse, out, stream) -> out
+PyObject* rotate_axes(PyObject* const* a) {
+  const Tensor &x = tensor(a[0]), &pos = tensor(a[1]);
+  const Axes axes(a[2]);
+  dtype_code(x);
+  if (x.dim() != 4) raise(PyExc_ValueError, "x: expected a [batch, head, row, head_dim] tensor");
+  const int64_t B = x.size(0), C = x.size(2), D = x.size(3);
+  heads_tensor(x, "x", B, C, D, x.scalar_type());
+  fits_axes(axes, D);
+  seco_desc d = axes_desc(B, C, D, x.scalar_type(), 0, "rope_rotate_axes");
+  int64_t ps[3];
+  positions_of(pos, axes, B, C, ps);
+  const int inv = PyObject_IsTrue(a[3]);
+  if (inv < 0) throw Raised{};
+  if (a[4] != Py_None) {
+    const Tensor& o = tensor(a[4]);
+    heads_tensor(o, "out", B, C, D, x.scalar_type());
+    writable(o, "out");
+    if (o.size(1) != x.size(1)) raise(PyExc_ValueError, "out must have the shape of x");
+    same_gpu(x, o);
+  }
+  same_gpu(x, pos);
+  OnGpu on(x, a[5]);
+  const Tensor out = a[4] == Py_None ? at::empty_like(x, x.options().requires_grad(false)) : tensor(a[4]);
+  heads_strides(x, d.q_stride);
+  heads_strides(out, d.o_stride);
+  if (x.numel() > 0)
+    check(lib.rope_rotate_axes(&d, &axes.x, (int32_t)x.size(1), ptr(x), ptr(out), static_cast<const int64_t*>(ptr(pos)), ps, inv, on.s),
+          "rope_rotate_axes");
+  return out_ref(a[4], out);
+}
+
+// (q or None, k_new, v_new, k_cache, v_cache, row_begin, positions, axes, q_out, stream) -> q_out or None
+PyObject* append_axes(PyObject* const* a) {
+  const Tensor* q = opt_tensor(a[0]);
+  const Tensor &kn = tensor(a[1]), &vn = tensor(a[2]), &kc = tensor(a[3]), &vc = tensor(a[4]), &pos = tensor(a[6]);
+  const Axes axes(a[7]);
+  const int64_t row = integer(a[5]);
+  dtype_code(kn);
+  if (kn.dim() != 4) raise(PyExc_ValueError, "k_new: expected a [batch, head, row, head_dim] tensor");
+  const int64_t B = kn.size(0), Hkv = kn.size(1), C = kn.size(2), D = kn.size(3);
+  heads_tensor(kn, "k_new", B, C, D, kn.scalar_type());
+  fits_axes(axes, D);
+  like_each_other(kn, vn, "k_new and v_new");
+  like_each_other(kc, vc, "k_cache and v_cache");
+  rows_inside(kc, "k_cache", B, Hkv, D, row, C, kn.scalar_type());
+  writable(kc, "k_cache");
+  if (q) heads_tensor(*q, "q", B, C, D, kn.scalar_type());
+  seco_desc d = axes_desc(B, C, D, kn.scalar_type(), row, "rope_append_axes");
+  int64_t ps[3];
+  positions_of(pos, axes, B, C, ps);
+  if (a[8] != Py_None) {
+    const Tensor& o = tensor(a[8]);
+    heads_tensor(o, "q_out", B, C, D, kn.scalar_type());
+    writable(o, "q_out");
+    if (!q || o.size(1) != q->size(1)) raise(PyExc_ValueError, "q_out must have the shape of q");
+    same_gpu(kn, o);
+  }
+  for (const Tensor* t : {&vn, &kc, &vc, &pos, q})
+    if (t) same_gpu(kn, *t);
+  OnGpu on(kn, a[9]);
+  Tensor out;
+  if (q) out = a[8] == Py_None ? at::empty_like(*q, q->options().requires_grad(false)) : tensor(a[8]);
+  d.n_kv_heads = (int32_t)Hkv;
+  heads_strides(kn, d.g_stride);
+  heads_strides(kc, d.kv_stride);
+  if (q) {
+    d.n_q_heads = (int32_t)q->size(1);
+    heads_strides(*q, d.q_stride);
+    heads_strides(out, d.o_stride);
+  }
+  if (kn.numel() > 0)
+    check(lib.rope_append_axes(&d, &axes.x, ptr(q), q ? ptr(out) : nullptr, ptr(kn), ptr(vn), ptr(kc), ptr(vc),
+                               static_cast<const int64_t*>(ptr(pos)), ps, on.s), "rope_append_axes");
+  if (!q) Py_RETURN_NONE;
+  return out_ref(a[8], out);
+}
+
+// (d_q or None, gk, gv, row_begin, positions, axes, scaler, dq_out, d_k, d_v, dtype or None, stream) -> (dq_out or None, d_k, d_v)
+PyObject* readout_axes(PyObject* const* a) {
+  const Tensor *dq = opt_tensor(a[0]), *dk_given = opt_tensor(a[8]), *dv_given = opt_tensor(a[9]);
+  const Tensor &gk = tensor(a[1]), &gv = tensor(a[2]), &pos = tensor(a[4]);
+  const Axes axes(a[5]);
+  const int64_t row = integer(a[3]);
+  if (gk.dim() != 4 || pos.dim() != 3) raise(PyExc_ValueError, "expected [batch, head, row, head_dim] buffers and [axes, batch, row] positions");
+  const int64_t B = gk.size(0), Hkv = gk.size(1), D = gk.size(3), C = pos.size(2);
+  at::ScalarType type;
+  if (a[10] != Py_None) {
+    if (!THPDtype_Check(a[10])) raise(PyExc_TypeError, "dtype must be a torch dtype");
+    type = reinterpret_cast<THPDtype*>(a[10])->scalar_type;
+  } else if (dq || dk_given) {
+    type = (dq ? *dq : *dk_given).scalar_type();
+  } else {
+    raise(PyExc_ValueError, "dtype: needed where neither d_q nor d_k is given");
+  }
+  if (type != at::kBFloat16 && type != at::kFloat) raise(PyExc_TypeError, "unsupported dtype: expected bfloat16 or float32");
+  like_each_other(gk, gv, "gk and gv");
+  rows_inside(gk, "gk", B, Hkv, D, row, C, at::kFloat);
+  fits_axes(axes, D);
+  if (dq) heads_tensor(*dq, "d_q", B, C, D, type);
+  if ((dk_given == nullptr) != (dv_given == nullptr)) raise(PyExc_ValueError, "d_k and d_v go together");
+  if (dk_given) {
+    like_each_other(*dk_given, *dv_given, "d_k and d_v");
+    heads_tensor(*dk_given, "d_k", B, C, D, type);
+    writable(*dk_given, "d_k");
+    if (dk_given->size(1) != Hkv) raise(PyExc_ValueError, "d_k must have the heads of gk");
+  }
+  seco_desc d = axes_desc(B, C, D, type, row, "rope_readout_axes");
+  int64_t ps[3];
+  positions_of(pos, axes, B, C, ps);
+  if (a[7] != Py_None) {
+    const Tensor& o = tensor(a[7]);
+    heads_tensor(o, "dq_out", B, C, D, type);
+    writable(o, "dq_out");
+    if (!dq || o.size(1) != dq->size(1)) raise(PyExc_ValueError, "dq_out must have the shape of d_q");
+    same_gpu(gk, o);
+  }
+  for (const Tensor* t : {&gv, &pos, dq, dk_given, dv_given})
+    if (t) same_gpu(gk, *t);
+  OnGpu on(gk, a[11]);
+  Tensor out, dk, dv;
+  if (dq) out = a[7] == Py_None ? at::empty_like(*dq, dq->options().requires_grad(false)) : tensor(a[7]);
+  if (dk_given) {
+    dk = *dk_given;
+    dv = *dv_given;
+  } else {
+    dk = at::empty({B, Hkv, C, D}, gk.options().dtype(type).requires_grad(false));
+    dv = at::empty_like(dk);
+  }
+  d.n_kv_heads = (int32_t)Hkv;
+  heads_strides(gk, d.g_stride);
+  heads_strides(dk, d.kv_stride);
+  if (dq) {
+    d.n_q_heads = (int32_t)dq->size(1);
+    heads_strides(*dq, d.q_stride);
+    heads_strides(out, d.o_stride);
+  }
+  if (dk.numel() > 0)
+    check(lib.rope_readout_axes(&d, &axes.x, ptr(dq), dq ? ptr(out) : nullptr, fptr(gk), fptr(gv), ptr(dk), ptr(dv), (float)real(a[6]),
+                                static_cast<const int64_t*>(ptr(pos)), ps, on.s), "rope_readout_axes");
+  PyObject* first = dq ? out_ref(a[7], out) : (Py_INCREF(Py_None), Py_None);
+  return Py_BuildValue("NNN", first, out_ref(a[8], dk), out_ref(a[9], dv));
+}
+
 }  // namespace
 
-PyMethodDef train_methods[] = {SECO_METHOD("adamw", adamw, 15), SECO_METHOD("norm_fwd", norm_fwd, 8), SECO_METHOD("norm_bwd", norm_bwd, 11), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef train_methods[] = {SECO_METHOD("rotate_axes", rotate_axes, 6), SECO_METHOD("append_axes", append_axes, 10),
+                               SECO_METHOD("readout_axes", readout_axes, 12), SECO_METHOD("adamw", adamw, 15), SECO_METHOD("norm_fwd", norm_fwd, 8), SECO_METHOD("norm_bwd", norm_bwd, 11), {nullptr, nullptr, 0, nullptr}};
 
 }  // namespace seco_ext
