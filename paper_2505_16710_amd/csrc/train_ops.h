@@ -79,7 +79,7 @@ struct RopeAxesArgs {
   RopePart q, k, v;                            // q, k: turned; v: as it is (heads 0: not there)
   const int64_t* positions;
   int64_t ps[3];                               // (axis, batch, row) strides
-  int B, C, D, n_axes;
+  int B, C, D, n_axes, slabs;                  // slabs: the launcher's
   float scale;                                 // of k and v
 };
 // bf16: the type of q and of what k and v give; wide_in: k and v are fp32 all the same

@@ -1,8 +1,8 @@
 """Rotary positions with several axes (csrc/rope_axes.hip) against a complex product in 64 bits on the CPU.
 
 Tolerances: angles and products are fp64, so that a result is its exact value rounded to fp32 and then to the storage type: half
-a step of that (2^-8 in bf16, 2^-24 in fp32) and 2^-24 of the pair's length (the first rounding), and 2^-40 of the pair's length for an
-angle of up to 2^34 that fp64 holds to 2^-18 ... of one at the positions used here (below 2^21) to 2^-31: 2^-30 of it."""
+a step of that (2^-8 in bf16, 2^-24 in fp32), 2^-24 of the pair's length for the first rounding, and 2^-30 of it for an angle of up to
+2^21, which fp64 and the frequency behind it hold to 2^-31."""
 import ctypes as C
 import math
 
@@ -199,6 +199,19 @@ def test_far_positions_and_far_rows():
     seco.rope_append_axes(None, kn, kn, kc, vc, row, p20, axes)
     assert torch.equal(kc[:, :, row:row + 20], seco.rope_rotate_axes(kn, p20, axes)) and torch.equal(vc[:, :, row:row + 20], kn)
     assert not kc[:, :, :row].any() and not kc[:, :, row + 20:].any() and not vc[:, :, row + 20:].any()
+
+
+@pytest.mark.gpu
+def test_more_rows_than_a_grid_holds_along_y():
+    """8 rows of head_dim 256 to a workgroup, 65535 of these along a dimension of the grid: the rows behind them, two batches."""
+    rows = 8 * 65535 + 11
+    axes = seco.RopeAxes((64, 64), BASE)
+    x = torch.zeros(2, 1, rows, 256, dtype=torch.bfloat16, device=DEV)
+    pos = torch.zeros(2, 1, rows, dtype=torch.int64, device=DEV)
+    x[:, :, -20:] = _rows(1, 2, 1, 20, 256, dtype=torch.bfloat16).to(DEV)
+    pos[:, :, -20:] = _positions(2, 2, 1, 20).to(DEV)
+    got = seco.rope_rotate_axes(x, pos, axes)
+    assert torch.equal(got[:, :, -20:], seco.rope_rotate_axes(x[:, :, -20:], pos[:, :, -20:], axes)) and not got[:, :, :-20].any()
 
 
 @pytest.mark.gpu
