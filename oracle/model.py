@@ -43,6 +43,10 @@ class ModelConfig:
     d_ff: int = 48
     vocab: int = 17
     rope_base: float = 0.0     # > 1: rotary position embedding of queries and keys with this base; 0: none
+    rope_sections: tuple = ()  # pairs of each axis of positions with several (rope_base then too); (): one axis, the row
+    rope_interleaved: bool = False
+    layer_norm: bool = False   # layer norms with the biases norm_f_b, l{l}.norm1_b, l{l}.norm2_b (where there are any)
+    norm_eps: float = 1e-5     # of the layer norms
 
     @property
     def scale(self):
@@ -71,6 +75,31 @@ def init_params(cfg: ModelConfig, seed: int, dtype=torch.float64):
 
 def _rmsnorm(x, g):
     return x * torch.rsqrt((x * x).mean(dim=-1, keepdim=True) + 1e-6) * g
+
+
+def _norm(cfg, params, name, x):
+    if not cfg.layer_norm:
+        return _rmsnorm(x, params[name])
+    x = x - x.mean(dim=-1, keepdim=True)
+    y = x * torch.rsqrt((x * x).mean(dim=-1, keepdim=True) + cfg.norm_eps) * params[name]
+    return y + params[name + "_b"] if name + "_b" in params else y
+
+
+def _rope_axes(cfg, x, pos):
+    """Rotary embedding of x [B,H,C,D] with several axes: pos [axes, B, C]; pair i belongs to the axis whose section holds it, or
+    (interleaved) to the next axis in turn that has pairs left; its frequency is base^(-2i/D)."""
+    D, left, axis = x.shape[-1], list(cfg.rope_sections), []
+    if not cfg.rope_interleaved:
+        axis = [a for a, n in enumerate(left) for _ in range(n)]
+    while len(axis) < D // 2:
+        for a in range(len(left)):
+            if left[a] > 0:
+                axis.append(a)
+                left[a] -= 1
+    th = torch.stack([pos[a].to(torch.float64) * float(cfg.rope_base) ** (-2.0 * i / D) for i, a in enumerate(axis)], -1)[:, None]
+    cos, sin = torch.cos(th).to(x.dtype), torch.sin(th).to(x.dtype)
+    a, b = x[..., :D // 2], x[..., D // 2:]
+    return torch.cat([a * cos - b * sin, b * cos + a * sin], dim=-1)
 
 
 def _rope(x, pos0, base):
@@ -102,29 +131,32 @@ def _attend(q, k_all, v_all, q_start, scale, col_w=None):
     return torch.einsum("bhrc,bhcd->bhrd", p, v_all.repeat_interleave(G, 1))
 
 
-def _chunk_forward(cfg, params, tokens, targets, q_start, caches, col_w=None):
+def _chunk_forward(cfg, params, tokens, targets, q_start, caches, col_w=None, positions=None):
     """One chunk through all layers (Eq. 1): returns (J_j, [(k_l, v_l)] of this chunk).
 
     caches[l] = (K_prefix, V_prefix) of the earlier chunks at layer l, [B,Hkv,q_start,D] (may be empty);
-    col_w[l] = per-column weights of layer l's dQ (see _attend), or None."""
+    col_w[l] = per-column weights of layer l's dQ (see _attend), or None; positions [axes, B, N]: of the whole sequence."""
     B, C = tokens.shape
     x = params["emb"][tokens]
     new_kv = []
     for l in range(cfg.n_layers):
-        h = _rmsnorm(x, params[f"l{l}.norm1"])
+        h = _norm(cfg, params, f"l{l}.norm1", x)
         q = (h @ params[f"l{l}.wq"]).view(B, C, cfg.n_q_heads, cfg.head_dim).transpose(1, 2)
         k = (h @ params[f"l{l}.wk"]).view(B, C, cfg.n_kv_heads, cfg.head_dim).transpose(1, 2)
         v = (h @ params[f"l{l}.wv"]).view(B, C, cfg.n_kv_heads, cfg.head_dim).transpose(1, 2)
-        if cfg.rope_base > 1.0:
+        if cfg.rope_sections:
+            here = positions[:, :, q_start:q_start + C].expand(-1, B, -1)
+            q, k = _rope_axes(cfg, q, here), _rope_axes(cfg, k, here)
+        elif cfg.rope_base > 1.0:
             q, k = _rope(q, q_start, cfg.rope_base), _rope(k, q_start, cfg.rope_base)
         new_kv.append((k, v))
         k_all = torch.cat([caches[l][0], k], dim=2)
         v_all = torch.cat([caches[l][1], v], dim=2)
         o = _attend(q, k_all, v_all, q_start, cfg.scale, None if col_w is None else col_w[l])
         x = x + o.transpose(1, 2).reshape(B, C, -1) @ params[f"l{l}.wo"]
-        h = _rmsnorm(x, params[f"l{l}.norm2"])
+        h = _norm(cfg, params, f"l{l}.norm2", x)
         x = x + F.silu(h @ params[f"l{l}.w1"]) @ params[f"l{l}.w2"]
-    logits = _rmsnorm(x, params["norm_f"]) @ params["head"]
+    logits = _norm(cfg, params, "norm_f", x) @ params["head"]
     loss = F.cross_entropy(logits.reshape(B * C, -1), targets.reshape(B * C), reduction="sum")
     return loss, new_kv
 
@@ -143,15 +175,16 @@ def _collect(params):
     return {n: (t.grad.clone() if t.grad is not None else torch.zeros_like(t)) for n, t in params.items()}
 
 
-def monolithic_grads(cfg, params, tokens, targets):
-    """Loss and parameter gradients of the whole sequence processed at once."""
+def monolithic_grads(cfg, params, tokens, targets, positions=None):
+    """Loss and parameter gradients of the whole sequence processed at once (positions: [axes, B or 1, N] under rope_sections)."""
     _zero_grads(params)
-    loss, _ = _chunk_forward(cfg, params, tokens, targets, 0, _empty_caches(cfg, tokens.shape[0], params["emb"].dtype))
+    loss, _ = _chunk_forward(cfg, params, tokens, targets, 0, _empty_caches(cfg, tokens.shape[0], params["emb"].dtype),
+                             positions=positions)
     loss.backward()
     return loss.detach(), _collect(params)
 
 
-def _stage1(cfg, params, tokens, targets, chunk_len):
+def _stage1(cfg, params, tokens, targets, chunk_len, positions=None):
     """Alg. 1 / Alg. 2, first loop: all chunks in inference mode; returns the checkpoints
     ckpt[j][l] = (K, V) of chunk j at layer l as detached leaves that can collect gradient."""
     B, N = tokens.shape
@@ -160,7 +193,8 @@ def _stage1(cfg, params, tokens, targets, chunk_len):
         for s0 in range(0, N, chunk_len):
             caches = [(torch.cat([c[l][0] for c in ckpt], 2), torch.cat([c[l][1] for c in ckpt], 2)) if ckpt
                       else _empty_caches(cfg, B, params["emb"].dtype)[l] for l in range(cfg.n_layers)]
-            loss, new_kv = _chunk_forward(cfg, params, tokens[:, s0:s0 + chunk_len], targets[:, s0:s0 + chunk_len], s0, caches)
+            loss, new_kv = _chunk_forward(cfg, params, tokens[:, s0:s0 + chunk_len], targets[:, s0:s0 + chunk_len], s0, caches,
+                                          positions=positions)
             total += float(loss)
             ckpt.append([(k.detach().clone(), v.detach().clone()) for k, v in new_kv])
     for c in ckpt:
@@ -170,7 +204,7 @@ def _stage1(cfg, params, tokens, targets, chunk_len):
     return ckpt, total
 
 
-def _stage2(cfg, params, tokens, targets, chunk_len, ckpt, order, factor, dq_weights=None):
+def _stage2(cfg, params, tokens, targets, chunk_len, ckpt, order, factor, dq_weights=None, positions=None):
     """Second loop: for every chunk in `order` (descending) rebuild its graph against the checkpoints,
     hand factor * m'_i.grad to the recomputed m_i and back-propagate J_i.
     dq_weights(i, l) -> one weight per chunk 0..i for the dQ of layer l in the call of chunk i (or None)."""
@@ -189,7 +223,7 @@ def _stage2(cfg, params, tokens, targets, chunk_len, ckpt, order, factor, dq_wei
                 col_w.append(None if w is None else torch.cat(
                     [torch.full((n,), float(x), dtype=params["emb"].dtype) for n, x in zip(lens, w)]))
         loss, new_kv = _chunk_forward(cfg, params, tokens[:, s0:s0 + chunk_len], targets[:, s0:s0 + chunk_len], s0, caches,
-                                      col_w)
+                                      col_w, positions)
         roots, grads = [loss], [torch.ones_like(loss)]
         for l, (k, v) in enumerate(new_kv):
             gk, gv = ckpt[i][l][0].grad, ckpt[i][l][1].grad
@@ -207,10 +241,10 @@ def seco_grads(cfg, params, tokens, targets, chunk_len, dq_weights=None):
     return total, _collect(params)
 
 
-def spaco_grads(cfg, params, tokens, targets, chunk_len, selected, factor, dq_weights=None):
+def spaco_grads(cfg, params, tokens, targets, chunk_len, selected, factor, dq_weights=None, positions=None):
     """Alg. 2: back-propagate only the selected chunks, relayed KV gradient scaled by `factor`."""
     _zero_grads(params)
-    ckpt, total = _stage1(cfg, params, tokens, targets, chunk_len)
+    ckpt, total = _stage1(cfg, params, tokens, targets, chunk_len, positions)
     _stage2(cfg, params, tokens, targets, chunk_len, ckpt, sorted({int(i) for i in selected}, reverse=True), float(factor),
-            dq_weights)
+            dq_weights, positions)
     return total, _collect(params)

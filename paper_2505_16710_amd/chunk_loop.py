@@ -27,6 +27,9 @@ Model (fixed here so that a checker can build the same function): pre-norm decod
 eps 1e-6, grouped-query causal attention (optionally with rotary position embedding), MLP x + silu(h W1) W2, final
 RMSNorm, linear head, cross-entropy summed over tokens.  Parameter names: emb, head, norm_f and
 l{i}.norm1, l{i}.norm2, l{i}.wq, l{i}.wk, l{i}.wv, l{i}.wo, l{i}.w1, l{i}.w2, all stored [in, out].
+With norm="layer" the norms are layer norms (rows minus their mean), whose biases are norm_f_b, l{i}.norm1_b and
+l{i}.norm2_b where params holds them; with rope_axes the rotary embedding has several axes (binding.RopeAxes) and step
+takes every token's positions on them.  optimizer.AdamW updates the parameters behind the step.
 """
 from __future__ import annotations
 
@@ -131,6 +134,45 @@ class Rope(torch.autograd.Function):
         return _b.rope_rotate(d_out.contiguous(), ctx.pos_start, ctx.base, inverse=True), None, None
 
 
+class RopeMulti(torch.autograd.Function):
+    """Rotary embedding with several axes (rope_rotate_axes) of x [B, H, C, D]; the gradient is turned back."""
+
+    @staticmethod
+    def forward(ctx, x, positions, axes):
+        ctx.axes = axes
+        ctx.save_for_backward(positions)
+        return _b.rope_rotate_axes(x.contiguous(), positions, axes)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_out):
+        return _b.rope_rotate_axes(d_out.contiguous(), ctx.saved_tensors[0], ctx.axes, inverse=True), None, None
+
+
+class LayerNorm(torch.autograd.Function):
+    """Layer norm of the rows of x [..., d] with gain and bias (or None): y, or, with a residual that is added first, (y, x +
+    residual), whose second result is what the next residual add takes."""
+
+    @staticmethod
+    def forward(ctx, x, gain, bias=None, eps=1e-5, residual=None):
+        y, mean, rstd, *out = _b.layer_norm_fwd(x, gain, bias, eps, residual)
+        ctx.save_for_backward(out[0] if out else x, gain, mean, rstd)
+        ctx.has_residual, ctx.has_bias = residual is not None, bias is not None
+        ctx.set_materialize_grads(False)
+        return (y, out[0]) if out else y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_y, d_sum=None):
+        x, gain, mean, rstd = ctx.saved_tensors
+        if d_y is None:                         # (only the sum was used)
+            return d_sum, None, None, None, d_sum if ctx.has_residual else None
+        d_x, d_gain, d_bias = _b.layer_norm_bwd(x, gain, mean, rstd, d_y.contiguous(), None if d_sum is None else d_sum.contiguous(),
+                                                with_gain=gain is not None and ctx.needs_input_grad[1],
+                                                with_bias=ctx.has_bias and ctx.needs_input_grad[2])
+        return d_x, d_gain, d_bias, None, d_x if ctx.has_residual else None
+
+
 def hand_over(params, grads):
     """Leaves every parameter's gradient in .grad (None there if no chunk reached it) and returns {name: gradient}, zeros
     for those.  A tensor under several names gets the sum over them.  A parameter that something waits for (hooks of
@@ -163,17 +205,27 @@ def hand_over(params, grads):
 
 
 class ChunkedDecoder:
-    """Holds the parameters (dict name -> leaf tensor on the GPU) and runs SeCO / SpaCO steps."""
+    """Holds the parameters (dict name -> leaf tensor on the GPU) and runs SeCO / SpaCO steps.
 
-    def __init__(self, params, n_layers, n_q_heads, n_kv_heads, head_dim, rope_base=None):
+    rope_base: base of the rotary embedding of queries and keys (keys are cached rotated), or None; rope_axes: a RopeAxes
+    instead, for positions with several axes.  norm: "rms", or "layer" with norm_eps."""
+
+    def __init__(self, params, n_layers, n_q_heads, n_kv_heads, head_dim, rope_base=None, norm="rms", norm_eps=1e-5, rope_axes=None):
+        if norm not in ("rms", "layer"):
+            raise ValueError("norm is 'rms' or 'layer'")
+        if rope_base is not None and rope_axes is not None:
+            raise ValueError("rope_base and rope_axes exclude each other")
+        if rope_axes is not None and rope_axes.head_dim != head_dim:
+            raise ValueError("rope_axes: the sections must add up to half of head_dim")
         self.p = params
-        self.rope_base = rope_base      # rotary embedding of queries and keys (keys are cached rotated), or None
+        self.rope_base, self.rope_axes = rope_base, rope_axes
+        self.norm, self.norm_eps = norm, norm_eps
         self.n_layers, self.Hq, self.Hkv, self.D = n_layers, n_q_heads, n_kv_heads, head_dim
         self.scale = float(head_dim) ** -0.5
         _b.load_library()          # fail here, loudly, if the HIP library has not been built
 
     def step(self, tokens, targets, chunk_len, selected=None, factor=1.0, keep_attention_outputs=False,
-             stage1_chunk_len=None, dq_weights=None, transposed_backward=False):
+             stage1_chunk_len=None, dq_weights=None, transposed_backward=False, positions=None, optimizer=None):
         """One SeCO step (selected is None: Alg. 1) or SpaCO step (Alg. 2, `selected` chunk indices,
         relay factor `factor`).  Returns (sum of the chunk losses, as stage 1 runs them, {name: gradient}).
 
@@ -197,7 +249,11 @@ class ChunkedDecoder:
         (spaco_chunk_attn_bwd_sparse_dq; not part of the paper).  For unbiased gradients the weights must have
         expectation 1 and be drawn independently for every layer of a call.
         transposed_backward: the attention backward in the transposed order (seco_chunk_attn_bwd_gather, under Alg. 2
-        spaco_chunk_attn_bwd_gather; bf16 parameters): same gradients up to the order of summation."""
+        spaco_chunk_attn_bwd_gather; bf16 parameters): same gradients up to the order of summation.
+        positions: with rope_axes, int64 [axes, batch or 1, tokens], every token's position on each axis (default: its number in
+        the sequence on all of them).
+        optimizer: an optimizer.AdamW over these parameters, whose step is taken with the step's gradients (not if a token lies
+        outside the table)."""
         p = self.p
         B, N = tokens.shape
         dtype, dev = p["emb"].dtype, p["emb"].device
@@ -208,6 +264,19 @@ class ChunkedDecoder:
                 raise TypeError("tokens and targets must be integers")
             if t.device != dev:
                 raise ValueError("tokens and targets must be on the parameters' device")
+        axes = None
+        if self.rope_axes is not None:
+            n_axes = len(self.rope_axes.sections)
+            if positions is None:
+                positions = torch.arange(N, device=dev).expand(n_axes, 1, N)
+            if positions.dtype != torch.int64 or positions.dim() != 3 or positions.shape[0] != n_axes or \
+                    positions.shape[1] not in (1, B) or positions.shape[2] < N:
+                raise ValueError("positions must be int64 [axes, batch or 1, tokens]")
+            if positions.device != dev:
+                raise ValueError("positions must be on the parameters' device")
+            axes = (self.rope_axes.packed, positions[:, :, :N].expand(n_axes, B, N))
+        elif positions is not None:
+            raise ValueError("positions go with rope_axes")
         starts = list(range(0, N, chunk_len))
         if transposed_backward:
             if dq_weights is not None or dtype != torch.bfloat16:
@@ -223,10 +292,14 @@ class ChunkedDecoder:
             raise ValueError("kept attention outputs: every chunk must lie within one chunk of stage 1")
         names = ["emb", "head", "norm_f"] + [f"l{l}.{n}" for l in range(self.n_layers)
                                              for n in ("norm1", "norm2", "wq", "wk", "wv", "wo", "w1", "w2")]
+        norms, biases = None, []
+        if self.norm == "layer":
+            biases = ["norm_f_b"] + [f"l{l}.{n}_b" for l in range(self.n_layers) for n in ("norm1", "norm2")]
+            norms = (self.norm_eps, [p.get(n) for n in biases])
         ext = _b._ext or _b._load_ext()
         with torch.no_grad():
             run = ext.step_new((self.n_layers, self.Hq, self.Hkv, self.D, self.scale, self.rope_base, B, N, min(c1, N),
-                                min(chunk_len, N), transposed_backward), [p[n] for n in names])
+                                min(chunk_len, N), transposed_backward, norms, axes), [p[n] for n in names])
             tokens, targets = tokens.to(torch.int64), targets.to(torch.int64)
             losses = torch.empty(N * B, dtype=torch.float32, device=dev)        # one per token, in stage-1 order
             # stage 2 rebuilds every chunk as stage 1 ran it, launch for launch: the losses come from there, and stage 1 ends
@@ -251,9 +324,12 @@ class ChunkedDecoder:
                 ext.step_train(run, tokens, targets, starts[j], min(starts[j] + chunk_len, N), keep_attention_outputs and j != once, w,
                                chunk_len, wq, losses if rebuilt or j == once else None)
             # (everything is on its way before the host waits for the loss)
-            result, grads = ext.step_result(run), dict(zip(names, ext.step_grads(run)))
+            result, grads = ext.step_result(run), dict(zip(names + biases, ext.step_grads(run)))
             torch.sum(losses, 0, out=result[0])
             total, outside = result.tolist()
         if outside:
             raise IndexError("tokens: an index is out of range of the embedding table")
-        return total, hand_over(p, grads)
+        grads = hand_over(p, grads)
+        if optimizer is not None:
+            optimizer.step()
+        return total, grads

@@ -27,7 +27,7 @@ using at::Tensor;
   X(dec_cross_entropy) X(dec_cross_entropy_both) X(dec_embedding_bwd) X(dec_gemm_supported) X(dec_gemm) X(dec_gemm_grads) X(dec_gemm_first_grads)      \
   X(dec_rope_qkv) X(dec_gemm_qkv) X(dec_gain_sums) X(dec_split_columns) X(dec_embed_rmsnorm_checked)              \
   X(layer_norm_fwd) X(layer_norm_bwd) X(layer_norm_workspace_bytes) X(adamw_step)                        \
-  X(rope_rotate_axes) X(rope_append_axes) X(rope_readout_axes)
+  X(rope_rotate_axes) X(rope_append_axes) X(rope_readout_axes) X(dec_add_layer_norm) X(dec_embed_layer_norm) X(dec_layer_norm_bwd)
 struct Lib {
 #define X(name) decltype(&::name) name = nullptr;
   SECO_ENTRIES(X)

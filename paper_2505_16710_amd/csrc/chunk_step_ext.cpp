@@ -6,6 +6,7 @@
 // 9.1 ms, of which the GPU worked 6.7; here a launch costs 2 - 4 us of host time, activations are carved from two
 // blocks allocated once per step, and the products are the library's own (gemm_bf16.hip) where type, alignment and size
 // allow: 3.4 ms, in which the GPU is busy throughout.
+#include <cstring>
 #include <map>
 #include <memory>
 
@@ -38,10 +39,16 @@ struct Param {
   at::ScalarType type = at::kFloat;              // type the norm computes its rows in)
 };
 
+// A norm's gain and, in a decoder of layer norms, bias (undefined: none), and the partial sums of their gradients
+struct Norm {
+  Param gain, bias;
+  float* part = nullptr;
+};
+
 struct Layer {
-  Param norm1, norm2, wqkv, wo, w1, w2;
+  Norm norm1, norm2;
+  Param wqkv, wo, w1, w2;
   int64_t ff = 0;                                // width of this layer's MLP
-  float *part1 = nullptr, *part2 = nullptr;      // partial sums of the gains' gradients
   Tensor k, v, gk, gv;                           // KV cache and KV-gradient buffers, [B, Hkv, N, D]
   std::map<int64_t, std::pair<Tensor, Tensor>> kept;   // q_start -> (O rows [B, C, Hq, D], LSE) of stage 1
   Tensor q_all, do_all, o_all, dq_all, stats;    // transposed backward order only
@@ -63,8 +70,13 @@ struct Step {
   size_t e;                                        // bytes per element
   int tail;                                        // type of the final norm's result, the head and the logits: dtype, or
                                                    // fp32 behind a bf16 body when both parameters are fp32
-  Param emb, head, norm_f;
-  float* part_f = nullptr;
+  Param emb, head;
+  Norm norm_f;
+  bool layer_norm = false;                         // else RMSNorm
+  float eps = 0.f;                                 // of the layer norms
+  bool axes = false;                               // rotary positions with several axes
+  rope_axes axis{};
+  Tensor positions;                                // their positions, int64 [axes, B, N] contiguous
   Tensor parts;
   Tensor result;                                   // the loss (the caller's sum), and 1 if a token lies outside the embedding table
   std::vector<Layer> layers;
@@ -176,8 +188,38 @@ struct Step {
     d.softmax_scale = (float)scale;
     return d;
   }
+  static const void* bias_of(const Norm& g) { return g.bias.w.defined() ? ptr(g.bias.w) : nullptr; }
   char* at_col(void* qkv, int64_t col) const { return static_cast<char*>(qkv) + col * (int64_t)e; }
+  // positions of rows q_start .. of the call, and their strides
+  const int64_t* places(int64_t q_start, int64_t (&st)[3]) const {
+    st[0] = positions.stride(0);
+    st[1] = positions.stride(1);
+    st[2] = 1;
+    return static_cast<const int64_t*>(ptr(positions)) + q_start;
+  }
+  // queries, and keys and values on their way to the cache or from gK / gV, under positions with several axes
+  void rope_axes_qkv(Layer& l, void* qkv, int64_t C, int64_t q_start, bool inverse) {
+    seco_desc d = desc(C, q_start, l);
+    int64_t ps[3];
+    const int64_t* pos = places(q_start, ps);
+    void *k = at_col(qkv, HD), *v = at_col(qkv, HD + Hkv * D);
+    std::copy(d.q_stride, d.q_stride + 3, d.o_stride);
+    if (inverse) {
+      std::copy(d.q_stride, d.q_stride + 3, d.kv_stride);
+      check(lib.rope_readout_axes(&d, &axis, qkv, qkv, fptr(l.gk), fptr(l.gv), k, v, 1.f, pos, ps, s), "rope_readout_axes");
+    } else {
+      std::copy(d.q_stride, d.q_stride + 3, d.g_stride);
+      check(lib.rope_append_axes(&d, &axis, qkv, qkv, k, v, ptr(l.k), ptr(l.v), pos, ps, s), "rope_append_axes");
+    }
+  }
   void rotate(void* qkv, int64_t C, int64_t q_start, bool inverse) {
+    if (axes) {
+      seco_desc d = desc(C, 0, layers[0]);
+      std::copy(d.q_stride, d.q_stride + 3, d.o_stride);
+      int64_t ps[3];
+      const int64_t* pos = places(q_start, ps);
+      return check(lib.rope_rotate_axes(&d, &axis, (int32_t)Hq, qkv, qkv, pos, ps, inverse, s), "rope_rotate_axes");
+    }
     if (rope_base == 0.0) return;
     seco_desc d = desc(C, 0, layers[0]);
     d.n_kv_heads = d.n_q_heads;
@@ -208,6 +250,7 @@ struct Step {
     append(l, qkv, C, q_start);
   }
   void append(Layer& l, void* qkv, int64_t C, int64_t q_start) {
+    if (axes) return rope_axes_qkv(l, qkv, C, q_start, false);
     if (rope_qkv(l, qkv, C, q_start, false)) return;
     rotate(qkv, C, q_start, false);
     seco_desc d = desc(C, q_start, l);
@@ -222,6 +265,7 @@ struct Step {
       check(lib.kv_append(&d, k, v, ptr(l.k), ptr(l.v), s), "kv_append");
   }
   void readout(Layer& l, void* d_qkv, int64_t C, int64_t q_start) {
+    if (axes) return rope_axes_qkv(l, d_qkv, C, q_start, true);
     if (rope_qkv(l, d_qkv, C, q_start, true)) return;
     rotate(d_qkv, C, q_start, true);
     seco_desc d = desc(C, q_start, l);
@@ -323,10 +367,14 @@ struct Step {
                 bool to_cache = false) {
     const int64_t R = B * C;
     auto rows = [&](int64_t n) { return mem.take((size_t)(R * n) * e); };
-    auto stats = [&]() { return static_cast<float*>(mem.take((size_t)R * 4)); };
-    auto norm = [&](void* x, void* y, const Param& g, void* xo, void* h, float* r) {
-      check(lib.dec_add_rmsnorm(dtype, x, y, ptr(g.w), xo, h, r, R, dm, s), "dec_add_rmsnorm");
+    auto stats = [&]() { return static_cast<float*>(mem.take((size_t)R * (layer_norm ? 8 : 4))); };   // rstd, mean
+    auto norm_of = [&](int type, void* x, void* y, const Norm& g, void* xo, void* h, float* r) {
+      if (layer_norm)
+        check(lib.dec_add_layer_norm(type, x, y, ptr(g.gain.w), bias_of(g), eps, xo, h, r + R, r, R, dm, s), "dec_add_layer_norm");
+      else
+        check(lib.dec_add_rmsnorm(type, x, y, ptr(g.gain.w), xo, h, r, R, dm, s), "dec_add_rmsnorm");
     };
+    auto norm = [&](void* x, void* y, const Norm& g, void* xo, void* h, float* r) { norm_of(dtype, x, y, g, xo, h, r); };
     // the chunk's rows of the table, written by the first norm
     x0 = layers.empty() ? at::index(emb.w, {tok}) : at::empty({R, dm}, opts());
     void *x = ptr(x0), *y = rows(dm), *logits = mem.take((size_t)(R * V) * head.w.element_size());
@@ -338,8 +386,11 @@ struct Step {
       sv.x1 = have_y && saved ? rows(dm) : x;
       sv.h1 = rows(dm);
       sv.r1 = stats();
-      if (&l == &layers.front())
-        check(lib.dec_embed_rmsnorm_checked(dtype, ptr(emb.w), static_cast<const int64_t*>(ptr(tok)), ptr(l.norm1.w), x, sv.h1, sv.r1, R, dm,
+      if (&l == &layers.front() && layer_norm)
+        check(lib.dec_embed_layer_norm(dtype, ptr(emb.w), static_cast<const int64_t*>(ptr(tok)), ptr(l.norm1.gain.w), bias_of(l.norm1), eps, x, sv.h1,
+                                       sv.r1 + R, sv.r1, R, dm, emb.w.size(0), fptr(result) + 1, s), "dec_embed_layer_norm");
+      else if (&l == &layers.front())
+        check(lib.dec_embed_rmsnorm_checked(dtype, ptr(emb.w), static_cast<const int64_t*>(ptr(tok)), ptr(l.norm1.gain.w), x, sv.h1, sv.r1, R, dm,
                                             emb.w.size(0), fptr(result) + 1, s), "dec_embed_rmsnorm");
       else
         norm(x, y, l.norm1, sv.x1, sv.h1, sv.r1);
@@ -377,7 +428,7 @@ struct Step {
       sv.keep_lse = at::empty_like(sv.keep_o);
       sv.x1 = ptr(sv.keep_o);
       sv.h1 = ptr(sv.keep_lse);
-      check(lib.dec_add_rmsnorm(tail, sv.x1, nullptr, ptr(norm_f.w), nullptr, sv.h1, sv.r1, R, dm, s), "dec_add_rmsnorm");
+      norm_of(tail, sv.x1, nullptr, norm_f, nullptr, sv.h1, sv.r1);
     }
     mm(logits, sv.h1, head, R);
     if (saved) saved->push_back(std::move(sv));
@@ -391,18 +442,22 @@ struct Step {
     auto rows = [&](int64_t n) { return mem.take((size_t)(R * n) * e); };
     void *dh = rows(dm), *dx = rows(dm), *du = rows(ff), *d_o = rows(HD), *d_qkv = rows(W);
     // dx <- dx + gradient of the norm at x (first: without dx)
-    auto norm_bwd = [&](void* x, const Param& g, float* r, float* part, bool first) {
-      check(lib.dec_rmsnorm_bwd(dtype, x, ptr(g.w), r, dh, first ? nullptr : dx, dx, part, R, dm, s), "dec_rmsnorm_bwd");
+    auto norm_grad = [&](int type, void* x, const Norm& g, float* r, void* d_h, void* d_in, void* d_x) {
+      if (layer_norm)
+        check(lib.dec_layer_norm_bwd(type, x, ptr(g.gain.w), r + R, r, d_h, d_in, d_x, g.part, R, dm, s), "dec_layer_norm_bwd");
+      else
+        check(lib.dec_rmsnorm_bwd(type, x, ptr(g.gain.w), r, d_h, d_in, d_x, g.part, R, dm, s), "dec_rmsnorm_bwd");
     };
+    auto norm_bwd = [&](void* x, const Norm& g, float* r, bool first) { norm_grad(dtype, x, g, r, dh, first ? nullptr : dx, dx); };
     const Saved fin = std::move(saved.back());
     saved.pop_back();
     if (tail == dtype) {
       grads(head, fin.h1, dh, d_logits, R);
-      norm_bwd(fin.x1, norm_f, fin.r1, part_f, true);
+      norm_bwd(fin.x1, norm_f, fin.r1, true);
     } else {
       const Tensor dh_f = at::empty_like(fin.keep_o), dx_f = at::empty_like(fin.keep_o);
       grads(head, fin.h1, ptr(dh_f), d_logits, R);
-      check(lib.dec_rmsnorm_bwd(tail, fin.x1, ptr(norm_f.w), fin.r1, ptr(dh_f), nullptr, ptr(dx_f), part_f, R, dm, s), "dec_rmsnorm_bwd");
+      norm_grad(tail, fin.x1, norm_f, fin.r1, ptr(dh_f), nullptr, ptr(dx_f));
       view(dx, {R, dm}).copy_(dx_f);
     }
     static const std::vector<float> none;
@@ -411,12 +466,12 @@ struct Step {
       const Saved& sv = saved[i];
       grads(l.w2, sv.a, du, dx, R, sv.u);
       grads(l.w1, sv.h2, dh, du, R);
-      norm_bwd(sv.x2, l.norm2, sv.r2, l.part2, false);
+      norm_bwd(sv.x2, l.norm2, sv.r2, false);
       grads(l.wo, sv.o, d_o, dx, R);
       attention_bwd(l, sv, d_o, d_qkv, C, q_start, w, wq.empty() ? none : wq[i], wlen);
       readout(l, d_qkv, C, q_start);
       grads(l.wqkv, sv.h1, dh, d_qkv, R);
-      norm_bwd(sv.x1, l.norm1, sv.r1, l.part1, false);
+      norm_bwd(sv.x1, l.norm1, sv.r1, false);
     }
     if (emb.wanted) {
       if (!emb.grad.defined()) emb.grad = at::zeros({emb.w.size(0), dm}, opts());
@@ -481,10 +536,13 @@ Param gain(PyObject* o, int64_t dm, at::ScalarType rows) {
   return p;
 }
 
-// (config, params): config = (n_layers, Hq, Hkv, D, scale, rope_base or None, B, N, chunk rows of stage 1, of stage 2, transposed);
+// (config, params): config = (n_layers, Hq, Hkv, D, scale, rope_base or None, B, N, chunk rows of stage 1, of stage 2, transposed),
+// behind them, if there, (eps, biases: [norm_f's, then norm1's, norm2's of every layer], None where there is none) of layer norms or None, and
+// (packed RopeAxes, positions) or None;
 // params = [emb, head, norm_f, then norm1, norm2, wq, wk, wv, wo, w1, w2 of every layer] -> step
 PyObject* step_new(PyObject* const* a) {
-  if (!PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 11 || !PyList_Check(a[1])) raise(PyExc_TypeError, "expected (tuple of 11, list)");
+  if (!PyTuple_Check(a[0]) || (PyTuple_GET_SIZE(a[0]) != 11 && PyTuple_GET_SIZE(a[0]) != 13) || !PyList_Check(a[1]))
+    raise(PyExc_TypeError, "expected (tuple of 11 or 13, list)");
   auto cfg = [&](int i) { return PyTuple_GET_ITEM(a[0], i); };
   auto st = std::make_unique<Step>();
   st->L = integer(cfg(0));
@@ -528,28 +586,68 @@ PyObject* step_new(PyObject* const* a) {
     for (int64_t k = 2; k < 8; ++k)
       if (at_layer(k).scalar_type() != body) raise(PyExc_TypeError, "parameters must share one dtype");
   }
+  PyObject *norms = PyTuple_GET_SIZE(a[0]) == 13 ? cfg(11) : Py_None, *rope = PyTuple_GET_SIZE(a[0]) == 13 ? cfg(12) : Py_None;
+  auto bias_at = [&](int64_t i) { return PyList_GET_ITEM(PyTuple_GET_ITEM(norms, 1), i); };
+  if (norms != Py_None) {
+    if (!PyTuple_Check(norms) || PyTuple_GET_SIZE(norms) != 2 || !PyList_Check(PyTuple_GET_ITEM(norms, 1)) ||
+        PyList_GET_SIZE(PyTuple_GET_ITEM(norms, 1)) != 1 + 2 * st->L)
+      raise(PyExc_TypeError, "layer norms: expected (eps, list of biases)");
+    st->layer_norm = true;
+    st->eps = (float)real(PyTuple_GET_ITEM(norms, 0));
+    if (!std::isfinite(st->eps) || st->eps < 0.f) raise(PyExc_ValueError, "the eps of a layer norm must be finite and not negative");
+    for (int64_t i = 0; i < 1 + 2 * st->L; ++i)
+      if (bias_at(i) != Py_None) {
+        const Tensor& b = tensor(bias_at(i));
+        check_gain(b, i == 0 ? "norm_f_b" : i % 2 ? "norm1_b" : "norm2_b", st->dm, i == 0 ? tail : body);
+        if (b.device() != first.device()) raise(PyExc_ValueError, "parameters must be on one GPU");
+      }
+  }
+  if (rope != Py_None) {
+    char* packed;
+    Py_ssize_t n;
+    if (!PyTuple_Check(rope) || PyTuple_GET_SIZE(rope) != 2) raise(PyExc_TypeError, "rotary axes: expected (packed RopeAxes, positions)");
+    if (PyBytes_AsStringAndSize(PyTuple_GET_ITEM(rope, 0), &packed, &n) < 0) throw Raised{};
+    if (n != (Py_ssize_t)sizeof(rope_axes)) raise(PyExc_TypeError, "rotary axes: expected (packed RopeAxes, positions)");
+    st->axes = true;
+    std::memcpy(&st->axis, packed, sizeof(rope_axes));
+    int64_t pairs = 0;
+    for (int i = 0; i < st->axis.n_axes && i < SECO_ROPE_MAX_AXES; ++i) pairs += st->axis.sections[i];
+    if (2 * pairs != st->D) raise(PyExc_ValueError, "rope_axes: the sections must add up to half of head_dim");
+    if (st->rope_base != 0.0) raise(PyExc_ValueError, "rope_base and rope_axes exclude each other");
+    const Tensor& t = tensor(PyTuple_GET_ITEM(rope, 1));
+    if (t.scalar_type() != at::kLong || t.dim() != 3 || t.size(0) != st->axis.n_axes || t.size(1) != st->B || t.size(2) != st->N)
+      raise(PyExc_ValueError, "positions: expected int64 [axes, batch, tokens]");
+    if (t.device() != first.device()) raise(PyExc_ValueError, "positions must be on the parameters' device");
+    st->positions = t.contiguous();
+  }
   for (int64_t i = 0; i < 3 + 8 * st->L; ++i)
     if (!tensor(par(i)).is_cuda() || tensor(par(i)).device() != first.device())
       raise(PyExc_ValueError, "parameters must be on one GPU");
   st->emb = param(par(0));
   st->head = param(par(1));
-  st->norm_f = gain(par(2), st->dm, tail);
+  st->norm_f.gain = gain(par(2), st->dm, tail);
+  auto set_bias = [&](Norm& n, int64_t i, at::ScalarType rows) {
+    if (st->layer_norm && bias_at(i) != Py_None) n.bias = gain(bias_at(i), st->dm, rows);
+  };
+  set_bias(st->norm_f, 0, tail);
   const Tensor& em = st->emb.w;
   st->e = em.element_size();
   st->V = st->head.w.size(1);
   st->ff = 0;
   const at::TensorOptions f32 = st->opts().dtype(at::kFloat);
-  const int64_t n_parts = (2 * st->L + 1) * DEC_GAIN_BLOCKS * st->dm;
+  const int64_t sets = st->layer_norm ? 2 : 1, n_parts = (2 * st->L + 1) * sets * DEC_GAIN_BLOCKS * st->dm;   // gains (and biases)
   st->parts = at::zeros({n_parts + 2}, f32);
   st->result = st->parts.slice(0, n_parts, n_parts + 2);
-  auto part = [&](int64_t i) { return fptr(st->parts) + i * DEC_GAIN_BLOCKS * st->dm; };
-  st->part_f = part(2 * st->L);
+  auto part = [&](int64_t i) { return fptr(st->parts) + i * sets * DEC_GAIN_BLOCKS * st->dm; };
+  st->norm_f.part = part(2 * st->L);
   st->layers.resize(st->L);
   for (int64_t i = 0; i < st->L; ++i) {
     Layer& l = st->layers[i];
     const int64_t p0 = 3 + 8 * i;
-    l.norm1 = gain(par(p0), st->dm, body);
-    l.norm2 = gain(par(p0 + 1), st->dm, body);
+    l.norm1.gain = gain(par(p0), st->dm, body);
+    l.norm2.gain = gain(par(p0 + 1), st->dm, body);
+    set_bias(l.norm1, 1 + 2 * i, body);
+    set_bias(l.norm2, 2 + 2 * i, body);
     // one projection product (and one gradient product each way) for queries, keys and values instead of three
     const Tensor &q = tensor(par(p0 + 2)), &k = tensor(par(p0 + 3)), &v = tensor(par(p0 + 4));
     l.wqkv.w = at::cat({q.detach(), k.detach(), v.detach()}, 1);
@@ -559,8 +657,8 @@ PyObject* step_new(PyObject* const* a) {
     l.w2 = param(par(p0 + 7));
     l.ff = l.w1.w.size(1);
     st->ff = std::max(st->ff, l.ff);
-    l.part1 = part(2 * i);
-    l.part2 = part(2 * i + 1);
+    l.norm1.part = part(2 * i);
+    l.norm2.part = part(2 * i + 1);
     // (cache rows are written before they are read; the gradient rows are cleared before stage 2)
     l.k = at::empty({st->B, st->Hkv, st->N, st->D}, st->opts());
     l.v = at::empty_like(l.k);
@@ -573,8 +671,8 @@ PyObject* step_new(PyObject* const* a) {
   }
   // activations: see forward / backward for what is taken (each piece rounded up to 256 bytes)
   const size_t e = st->e;
-  auto layer_bytes = [&](int64_t R) { return (size_t)R * ((4 * st->dm + st->W + st->HD + 2 * st->ff) * e + 8 + 4 * st->Hq) + 12 * 256; };
-  auto other_bytes = [&](int64_t R) { return (size_t)R * (3 * st->dm * e + st->V * st->head.w.element_size() + 4) + 8 * 256; };
+  auto layer_bytes = [&](int64_t R) { return (size_t)R * ((4 * st->dm + st->W + st->HD + 2 * st->ff) * e + 8 * sets + 4 * st->Hq) + 12 * 256; };
+  auto other_bytes = [&](int64_t R) { return (size_t)R * (3 * st->dm * e + st->V * st->head.w.element_size() + 4 * sets) + 8 * 256; };
   auto bwd_bytes = [&](int64_t R) { return (size_t)R * (2 * st->dm + st->ff + st->HD + st->W) * e + 8 * 256; };
   const int64_t R1 = st->B * c1, R2 = st->B * c2;
   st->stage1.create(layer_bytes(R1) + other_bytes(R1), em);
@@ -665,16 +763,19 @@ PyObject* step_train(PyObject* const* a) {
 // (step) -> fp32 [2]: room for the loss, and 1 if a token of a chunk so far lies outside the embedding table, else 0
 PyObject* step_result(PyObject* const* a) { return THPVariable_Wrap(step_of(a[0]).result); }
 
-// (step) -> gradients in the order of step_new's params; None where no chunk reached the parameter
+// (step) -> gradients in the order of step_new's params, then, in a decoder of layer norms, of its biases; None where no chunk
+// reached the parameter, or there is none
 PyObject* step_grads(PyObject* const* a) {
   Step& st = step_of(a[0]);
   begin(st);
   std::vector<Tensor> out = {st.emb.grad, st.head.grad};
-  const Tensor sums = at::empty({2 * st.L + 1, st.dm}, st.parts.options()), gains = st.dtype == SECO_F32 ? sums : at::empty({2 * st.L + 1, st.dm}, st.opts());
-  check(lib.dec_gain_sums(st.dtype, fptr(st.parts), fptr(sums), st.dtype == SECO_F32 ? nullptr : ptr(gains), 2 * st.L + 1, st.dm, st.s),
+  const int64_t sets = st.layer_norm ? 2 : 1, n_sums = (2 * st.L + 1) * sets;      // a norm's gain (and bias) behind the other
+  const Tensor sums = at::empty({n_sums, st.dm}, st.parts.options()), gains = st.dtype == SECO_F32 ? sums : at::empty({n_sums, st.dm}, st.opts());
+  check(lib.dec_gain_sums(st.dtype, fptr(st.parts), fptr(sums), st.dtype == SECO_F32 ? nullptr : ptr(gains), n_sums, st.dm, st.s),
         "dec_gain_sums");
-  auto gain = [&](int64_t i, const Param& p) {
-    if (!st.trained) return Tensor();
+  auto gain = [&](int64_t norm, const Param& p, bool bias = false) {
+    const int64_t i = norm * sets + bias;
+    if (!st.trained || !p.w.defined()) return Tensor();
     if (p.type == gains.scalar_type() && p.sizes.size() == 1 && p.sizes[0] == st.dm) return gains.select(0, i);
     Tensor g = sums.select(0, i);
     int64_t n = 1;
@@ -682,11 +783,11 @@ PyObject* step_grads(PyObject* const* a) {
     if (n != st.dm) g = g.sum();
     return g.to(p.type).reshape(p.sizes);
   };
-  out.push_back(gain(2 * st.L, st.norm_f));
+  out.push_back(gain(2 * st.L, st.norm_f.gain));
   for (int64_t i = 0; i < st.L; ++i) {
     Layer& l = st.layers[i];
-    out.push_back(gain(2 * i, l.norm1));
-    out.push_back(gain(2 * i + 1, l.norm2));
+    out.push_back(gain(2 * i, l.norm1.gain));
+    out.push_back(gain(2 * i + 1, l.norm2.gain));
     const int64_t kv = st.Hkv * st.D;
     Tensor q, k, v;
     if (l.wqkv.grad.defined()) {
@@ -700,6 +801,13 @@ PyObject* step_grads(PyObject* const* a) {
     out.push_back(l.wo.grad);
     out.push_back(l.w1.grad);
     out.push_back(l.w2.grad);
+  }
+  if (st.layer_norm) {
+    out.push_back(gain(2 * st.L, st.norm_f.bias, true));
+    for (int64_t i = 0; i < st.L; ++i) {
+      out.push_back(gain(2 * i, st.layers[i].norm1.bias, true));
+      out.push_back(gain(2 * i + 1, st.layers[i].norm2.bias, true));
+    }
   }
   PyObject* list = PyList_New((Py_ssize_t)out.size());
   if (!list) throw Raised{};

@@ -20,6 +20,14 @@ int dec_embed_rmsnorm_checked(int dtype, const void* table, const int64_t* token
 #define DEC_GAIN_BLOCKS 256
 int dec_rmsnorm_bwd(int dtype, const void* x, const void* gain, const float* rstd, const void* d_h, const void* d_in,
                     void* d_x, float* gain_part, int64_t rows, int64_t d, void* stream);
+// The same with a layer norm (layer_norm.hip; gain and bias, NULL: none, of dtype): h = (x_out - mean) rstd gain + bias, rstd = 1 / sqrt(var + eps);
+// y NULL: x_out is not written.  parts[2][DEC_GAIN_BLOCKS, d] += the shares of the gain's and of the bias's gradient
+int dec_add_layer_norm(int dtype, const void* x, const void* y, const void* gain, const void* bias, float eps, void* x_out, void* h, float* mean,
+                       float* rstd, int64_t rows, int64_t d, void* stream);
+int dec_embed_layer_norm(int dtype, const void* table, const int64_t* token, const void* gain, const void* bias, float eps, void* x_out, void* h,
+                         float* mean, float* rstd, int64_t rows, int64_t d, int64_t v, float* outside, void* stream);
+int dec_layer_norm_bwd(int dtype, const void* x, const void* gain, const float* mean, const float* rstd, const void* d_h, const void* d_in, void* d_x,
+                       float* parts, int64_t rows, int64_t d, void* stream);
 // sums[n, d] = parts[n, DEC_GAIN_BLOCKS, d] summed over the blocks in a fixed order; rounded (NULL: not written): the same in dtype
 int dec_gain_sums(int dtype, const float* parts, float* sums, void* rounded, int64_t n, int64_t d, void* stream);
 // src [rows, a + b + c bytes] -> a, b, c, each contiguous; sizes are multiples of 16 bytes

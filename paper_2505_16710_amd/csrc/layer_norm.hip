@@ -381,7 +381,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_rows_kernel(NormArgs a) {
   };
   float* part = a.parts + (int64_t)blockIdx.x * d;
   leave(c.dg, part);
-  leave(c.db, part + (int64_t)a.blocks * d);
+  leave(c.db, part + (int64_t)a.part_rows * d);
 }
 
 // A workgroup to a row, R rows at a time: one barrier for their 2 R sums.  AHEAD: the next rows are requested under the present
@@ -444,7 +444,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_block_kernel(NormArgs a) {
   }
   if (!a.parts) return;
   float* part = a.parts + (int64_t)blockIdx.x * d;
-  float* part_b = part + (int64_t)a.blocks * d;
+  float* part_b = part + (int64_t)a.part_rows * d;
 #pragma unroll
   for (int k = 0; k < KB; ++k)
 #pragma unroll
@@ -463,7 +463,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_long_kernel(NormArgs a) {
   const int64_t d = a.d;
   const float inv = 1.f / (float)d;
   float* part = a.parts ? a.parts + (int64_t)blockIdx.x * d : nullptr;
-  float* part_b = part ? part + (int64_t)a.blocks * d : nullptr;
+  float* part_b = part ? part + (int64_t)a.part_rows * d : nullptr;
   if (part && !a.accumulate)
     for (int64_t c = threadIdx.x; c < d; c += kBlock) part[c] = part_b[c] = 0.f;     // (each element is one thread's own)
   int turn = 0;

@@ -18,7 +18,8 @@ struct NormArgs {
   const void* dy;
   void *out, *y;                 // forward: x + r (NULL without r) and the result; backward: d_x in out
   float *mean, *rstd;
-  float *parts;                  // backward: [2][blocks][d] sums of d_gain and d_bias per workgroup, or NULL
+  float *parts;                  // backward: sums of d_gain per workgroup [blocks][d] and, part_rows rows on, of d_bias; or NULL
+  int part_rows;
   int64_t rows, d, xs, rs, os, ys;
   float eps;
   int dtype, gain_f32;           // gain_f32: gain and bias are fp32 (else of dtype)

@@ -2,7 +2,10 @@
 // nothing here allocates device memory, synchronises or keeps state between calls.
 #include <cmath>
 
+#include "decoder.h"
 #include "train_ops.h"
+
+static_assert(SECO_NORM_BLOCKS == DEC_GAIN_BLOCKS, "the training step adds up the shares of either norm");
 
 namespace seco {
 namespace {
@@ -85,12 +88,23 @@ int check_rope_axes(const seco_desc* d, const rope_axes* x, const int64_t* posit
 void fill_rope(RopeAxesArgs& a, const seco_desc* d, const rope_axes* x, const int64_t* positions, const int64_t* pos_stride) {
   const int pairs = d->head_dim / 2;
   int left[SECO_ROPE_MAX_AXES], seen[SECO_ROPE_MAX_AXES] = {};
-  for (int i = 0; i < x->n_axes; ++i) left[i] = x->sections[i];
+  // base^(-k / n) as a product of powers for the bits of k (an exponential for every pair was a third of a short call's host time)
+  double power[SECO_ROPE_MAX_AXES][7];
+  const double log2_base = std::log2((double)x->base);
+  for (int i = 0; i < x->n_axes; ++i) {
+    left[i] = x->sections[i];
+    const int n = x->own_frequencies ? x->sections[i] : pairs;
+    if (i == 0 || x->own_frequencies)
+      for (int j = 0; j < 7 && 1 << j < n; ++j) power[i][j] = std::exp2(-(double)(1 << j) / n * log2_base);
+  }
   for (int i = 0, axis = 0; i < pairs; ++i) {
     while (left[axis] == 0) axis = axis + 1 == x->n_axes ? 0 : axis + 1;   // (some axis lacks pairs: they add up)
     a.axis[i] = (uint8_t)axis;
-    const double of = x->own_frequencies ? (double)seen[axis] / x->sections[axis] : (double)i / pairs;
-    a.frequency[i] = std::exp2(-of * std::log2((double)x->base));
+    const double* of = power[x->own_frequencies ? axis : 0];
+    double f = 1.0;
+    for (int k = x->own_frequencies ? seen[axis] : i, j = 0; k; k >>= 1, ++j)
+      if (k & 1) f *= of[j];
+    a.frequency[i] = f;
     ++seen[axis];
     --left[axis];
     if (x->interleaved) axis = axis + 1 == x->n_axes ? 0 : axis + 1;
@@ -228,7 +242,7 @@ extern "C" int layer_norm_bwd(const layer_norm_desc* desc, const void* x, const 
   a.dy = d_y;
   a.out = d_x;
   a.parts = sums ? static_cast<float*>(ws) : nullptr;
-  a.blocks = norm_blocks(desc->rows, desc->d, desc->dtype);
+  a.blocks = a.part_rows = norm_blocks(desc->rows, desc->d, desc->dtype);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   rc = launch_norm_bwd(a, s);
   if (rc || !sums) return rc;
@@ -281,4 +295,68 @@ extern "C" int adamw_step(const adamw_desc* desc, const adamw_tensor* tensors_ho
   if (rc || (a.counted && !a.count)) return rc;
   a.last = !a.counted;
   return launch_adamw(pending, a, hs);
+}
+
+// ---- layer norm in the training step (decoder.h): contiguous rows, gain and bias of their type
+namespace {
+NormArgs step_norm(int dtype, const void* gain, const void* bias, float eps, int64_t rows, int64_t d) {
+  NormArgs a{};
+  a.rows = rows;
+  a.d = a.xs = a.rs = a.os = a.ys = d;
+  a.dtype = dtype;
+  a.gain_f32 = dtype == SECO_F32;
+  a.gain = gain;
+  a.bias = bias;
+  a.eps = eps;
+  return a;
+}
+bool step_sizes(int dtype, int64_t rows, int64_t d) { return is_dtype(dtype) && rows >= 0 && rows < (int64_t)1 << 31 && d >= 1 && d <= (int64_t)1 << 30; }
+}  // namespace
+
+extern "C" int dec_add_layer_norm(int dtype, const void* x, const void* y, const void* gain, const void* bias, float eps, void* x_out, void* h,
+                                  float* mean, float* rstd, int64_t rows, int64_t d, void* stream) {
+  if (!step_sizes(dtype, rows, d)) return SECO_ERR_SHAPE;
+  if (rows == 0) return SECO_OK;
+  NormArgs a = step_norm(dtype, gain, bias, eps, rows, d);
+  a.x = x;
+  a.r = y;
+  a.out = y ? x_out : nullptr;
+  a.y = h;
+  a.mean = mean;
+  a.rstd = rstd;
+  return launch_norm_fwd(a, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int dec_embed_layer_norm(int dtype, const void* table, const int64_t* token, const void* gain, const void* bias, float eps, void* x_out,
+                                    void* h, float* mean, float* rstd, int64_t rows, int64_t d, int64_t v, float* outside, void* stream) {
+  if (!step_sizes(dtype, rows, d) || v < 1) return SECO_ERR_SHAPE;
+  if (rows == 0) return SECO_OK;
+  NormArgs a = step_norm(dtype, gain, bias, eps, rows, d);
+  a.x = table;
+  a.token = token;
+  a.table = v;
+  a.outside = outside;
+  a.out = x_out;
+  a.y = h;
+  a.mean = mean;
+  a.rstd = rstd;
+  return launch_norm_fwd(a, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int dec_layer_norm_bwd(int dtype, const void* x, const void* gain, const float* mean, const float* rstd, const void* d_h,
+                                  const void* d_in, void* d_x, float* parts, int64_t rows, int64_t d, void* stream) {
+  if (!step_sizes(dtype, rows, d)) return SECO_ERR_SHAPE;
+  if (rows == 0) return SECO_OK;
+  NormArgs a = step_norm(dtype, gain, nullptr, 0.f, rows, d);
+  a.x = x;
+  a.r = d_in;
+  a.dy = d_h;
+  a.out = d_x;
+  a.mean = const_cast<float*>(mean);
+  a.rstd = const_cast<float*>(rstd);
+  a.parts = parts;
+  a.part_rows = SECO_NORM_BLOCKS;
+  a.blocks = norm_blocks(rows, d, dtype);
+  a.accumulate = 1;
+  return launch_norm_bwd(a, static_cast<hipStream_t>(stream));
 }

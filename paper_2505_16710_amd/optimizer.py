@@ -1,8 +1,8 @@
 """AdamW over a model's parameters: the state that `binding.adamw_step` updates, and one call per training step.
 
     opt = AdamW(params, lr=3e-4, weight_decay=0.1, state_bits=8)
-    loss, grads = decoder.step(tokens, targets, chunk_len)
-    opt.step(grads)                                             # or decoder.step(..., optimizer=opt)
+    loss, grads = decoder.step(tokens, targets, chunk_len)      # leaves the gradients in .grad
+    opt.step()                                                  # or decoder.step(..., optimizer=opt)
 
 Per parameter the state is m and v in fp32 (8 bytes) or in 8 bits (2.03 bytes), and for bf16 parameters, unless
 masters=False, an fp32 master (4 bytes).  Without a master a bf16 parameter is rounded after every step, and an update below
@@ -54,7 +54,8 @@ class AdamW:
 
     def step(self, grads=None, grad_scale=None):
         """One update.  grads: None (every parameter's .grad), or a dict by the names of the parameters, or a list in their
-        order; a parameter without a gradient (None, or not in the dict) stays as it is, its states too.  grad_scale: a
+        order; a parameter without a gradient (None, or not in the dict) stays as it is, its states too, while one whose
+        gradient is zero decays.  grad_scale: a
         one-element fp32 tensor on the GPU that the gradients are multiplied by (clipping, loss scaling), or None."""
         if grads is None:
             found = [t.grad for t in self.params]
