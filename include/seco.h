@@ -348,8 +348,8 @@ int rope_readout_axes(const seco_desc* desc, const rope_axes* axes, const void* 
  * stride).  d_in may be NULL (nothing is added); d_x may be x, d_y or d_in (same stride).  In the backward, x is the row that
  * was normalised: x_out where there was a residual.  d_gain, d_bias: overwritten; NULL: not wanted.
  * rows = 0 is allowed (d_gain and d_bias are then zeros).  Row strides of inputs may be 0 (one row for all).
- * ws of the backward: layer_norm_workspace_bytes(desc) bytes, 16-byte aligned; not needed when neither d_gain nor d_bias is
- * wanted.
+ * ws of the backward: layer_norm_workspace_bytes(desc) bytes, 16-byte aligned; not needed (NULL) where these are 0, or when
+ * neither d_gain nor d_bias is wanted.
  */
 typedef struct layer_norm_desc {
   int64_t rows, d;

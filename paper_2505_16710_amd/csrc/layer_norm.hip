@@ -535,6 +535,102 @@ __global__ __launch_bounds__(256) void norm_sums_kernel(const float* parts, int 
   to[c] = (T)s;
 }
 
+// A call of few rows: one launch, without parts.  The statistics are known, so that the sums of the columns need nothing from the
+// rows' workgroups (the first a.blocks): the ones behind them walk down the rows, 4 words of columns to a workgroup, 128
+// groups of lanes that take every 128th row each, four at a time, then a tree over the groups.  Two workgroups read a cache line
+// of 128 bytes: `which` puts them on one XCD (1024 x 8192 bf16 22.7 -> 18.4 us).
+template <typename T, int V> __device__ __forceinline__ void column_sums(const NormArgs& a, int which) {
+  __shared__ float sh[kBlock / 64][4][2][V];
+  constexpr int kGroups = kBlock / 4, kAhead = 4;
+  const int lane = threadIdx.x & 3, rows = (int)a.rows;
+  const Place<V, 4> at(which, lane, (int)a.d);
+  float s[2][V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) s[0][j] = s[1][j] = 0.f;
+  for (int r0 = threadIdx.x >> 2; r0 < rows; r0 += kAhead * kGroups) {
+    Pack<T, V> x[kAhead], y[kAhead];
+    float mean[kAhead], rstd[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int64_t r = r0 + i * kGroups < rows ? r0 + i * kGroups : r0;
+      x[i] = Pack<T, V>::at(static_cast<const T*>(a.x) + r * a.xs, at.at);
+      y[i] = Pack<T, V>::at(static_cast<const T*>(a.dy) + r * a.ys, at.at);
+      mean[i] = a.mean[r];
+      rstd[i] = a.rstd[r];
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const bool is = r0 + i * kGroups < rows;
+      float n[V], f[V];
+      x[i].get(n);
+      y[i].get(f);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        s[0][j] += is ? f[j] * ((n[j] - mean[i]) * rstd[i]) : 0.f;
+        s[1][j] += is ? f[j] : 0.f;
+      }
+    }
+  }
+  const int wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      float f = s[k][j];
+      f += with_partner<0x128>(f);                // lane i - 8 of the same 16, in turn
+      f += with_partner<0x124>(f);                // lane i - 4
+      f = sum_across_32(sum_across_16(f));
+      if ((threadIdx.x & 63) < 4) sh[wave][lane][k][j] = f;
+    }
+  __syncthreads();
+  if (threadIdx.x >= 8 * V) return;
+  const int l = threadIdx.x / (2 * V), k = threadIdx.x / V & 1, j = threadIdx.x % V;
+  const Place<V, 4> to(which, l, (int)a.d);
+  void* out = k ? a.d_bias : a.d_gain;
+  if (j < to.skip || !out) return;
+  float f = sh[0][l][k][j];
+#pragma unroll
+  for (int w = 1; w < kBlock / 64; ++w) f += sh[w][l][k][j];
+  if (sizeof(T) == 4 || a.gain_f32) static_cast<float*>(out)[to.at + j] = f;
+  else static_cast<T*>(out)[to.at + j] = (T)f;
+}
+template <typename T, int V, int G, int KB, bool IN>
+__global__ __launch_bounds__(kBlock) void norm_bwd_few_kernel(NormArgs a) {
+  __shared__ float sh[kBlock / 64][2];
+  if ((int)blockIdx.x >= a.blocks) {
+    const int b = (int)blockIdx.x - a.blocks, n = (int)gridDim.x - a.blocks;
+    return column_sums<T, V>(a, b < n / 16 * 16 ? b / 16 * 16 + b % 8 * 2 + b / 8 % 2 : b);
+  }
+  const int d = (int)a.d;
+  const Words<T, V, G, KB> at(threadIdx.x % G, d);
+  const int64_t row = row_of<G>((int64_t)blockIdx.x * (kBlock / G) + threadIdx.x / G);
+  if (row >= a.rows) return;                      // (a workgroup to a row: never)
+  Held<T, V, KB, 1, IN, false> now;
+  now.load(a, row, 1, at);
+  Columns<T, V, KB> c(a, at);
+  float s[2];
+  c.add(now.x[0], now.y[0], 0xffffffffu, now.mean[0], now.rstd[0], s[0], s[1]);
+  if constexpr (G > 64) {
+    block_sums<G, 2>(s, sh);
+  } else {
+    s[0] = lanes_sum<G>(s[0]);
+    s[1] = lanes_sum<G>(s[1]);
+  }
+  const float inv = 1.f / (float)d;
+  T* out = static_cast<T*>(a.out) + row * a.os;
+#pragma unroll
+  for (int k = 0; k < KB; ++k) {
+    float f[V], g[V];
+    c.word(k, now.x[0][k], now.y[0][k], now.mean[0], now.rstd[0], s[0] * inv, s[1] * inv, f);
+    if constexpr (IN) {
+      now.in[0][k].get(g);
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] += g[j];
+    }
+    if (at[k].skip < V) Pack<T, V>::of(f).to(out, at[k].at);
+  }
+}
+
 // f is called with the elements of a word, the lanes to a row and the words to a lane.
 template <int V, int G, int KB, typename F> bool take(F f) {
   f(std::integral_constant<int, V>{}, std::integral_constant<int, G>{}, std::integral_constant<int, KB>{});
@@ -632,7 +728,30 @@ template <typename T> int norm_bwd(const NormArgs& a, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? SECO_OK : SECO_ERR_LAUNCH;
 }
 
+template <typename T> int norm_bwd_few(NormArgs a, bool rows_too, hipStream_t s) {
+  backward_shape<T>(a.d, [&](auto v, auto g, auto kb) {
+    constexpr int V = decltype(v)::value, G = decltype(g)::value, KB = decltype(kb)::value, kRows = kBlock / G;
+    a.blocks = rows_too ? (int)((a.rows + kRows - 1) / kRows) : 0;
+    const unsigned grid = (unsigned)(a.blocks + (a.d + 4 * V - 1) / (4 * V));
+    if (a.r) hipLaunchKernelGGL((norm_bwd_few_kernel<T, V, G, KB, true>), dim3(grid), dim3(kBlock), 0, s, a);
+    else hipLaunchKernelGGL((norm_bwd_few_kernel<T, V, G, KB, false>), dim3(grid), dim3(kBlock), 0, s, a);
+  });
+  return hipGetLastError() == hipSuccess ? SECO_OK : SECO_ERR_LAUNCH;
+}
+
 }  // namespace
+
+// Up to 1024 rows (beyond, the walk down the rows is the longest way: 2048 x 45 bf16 10.5 us, by parts 7.0), while x and d_y are
+// held by the caches between the two readings: up to 16 MiB each.  us on the GPU, one launch / parts and their sums: bf16
+// 16 x 1024 3.4 / 8.3, 512 x 4096 6.1 / 14.2, 1024 x 8192 18.4 / 26.8; fp32 1024 x 4096 15.2 / 16.6, but 1024 x 8192 26.3 / 27.7 and
+// 2048 x 4096 30.5 / 23.5.
+bool norm_few(int64_t rows, int64_t d, int dtype) {
+  const int64_t elem = dtype == SECO_BF16 ? 2 : 4;
+  return rows >= 1 && rows <= 1024 && d * elem <= 32768 && rows * d * elem <= (int64_t)16 << 20;   // (32768: backward_shape's longest)
+}
+int launch_norm_bwd_few(const NormArgs& a, bool rows_too, hipStream_t s) {
+  return a.dtype == SECO_BF16 ? norm_bwd_few<__bf16>(a, rows_too, s) : norm_bwd_few<float>(a, rows_too, s);
+}
 
 int norm_blocks(int64_t rows, int64_t d, int dtype) {
   const int per = dtype == SECO_BF16 ? rows_of_block<__bf16>(d) : rows_of_block<float>(d);

@@ -23,6 +23,7 @@ struct NormArgs {
   int64_t rows, d, xs, rs, os, ys;
   float eps;
   int dtype, gain_f32;           // gain_f32: gain and bias are fp32 (else of dtype)
+  void *d_gain, *d_bias;         // backward of few rows: the sums themselves (either NULL)
   int blocks, accumulate;        // workgroups that leave sums; 1: they are added to what is there
   // forward, first norm of a decoder: row r of x is row token[r] of a table of `table` rows
   const int64_t* token;
@@ -32,6 +33,10 @@ struct NormArgs {
 int norm_blocks(int64_t rows, int64_t d, int dtype);                       // workgroups of a backward call
 int launch_norm_fwd(const NormArgs& a, hipStream_t s);
 int launch_norm_bwd(const NormArgs& a, hipStream_t s);
+// Whether a backward call has so few rows that its sums need no parts, but come from a.x and a.dy a second time; and that call:
+// the sums, and d_x with them unless it overwrites either
+bool norm_few(int64_t rows, int64_t d, int dtype);
+int launch_norm_bwd_few(const NormArgs& a, bool rows_too, hipStream_t s);
 // d_gain, d_bias (either NULL) = parts added up over the blocks in their order
 int launch_norm_sums(const float* parts, int blocks, int64_t d, void* d_gain, void* d_bias, int gain_f32, hipStream_t s);
 

@@ -40,6 +40,11 @@ NormArgs norm_args(const layer_norm_desc* d) {
   a.gain_f32 = d->gain_dtype == SECO_F32;
   return a;
 }
+// whether the rows of d_x and of another tensor share memory, or may
+bool overlap(const layer_norm_desc* d, const void* d_x, const void* other, int64_t stride) {
+  const uintptr_t e = (uintptr_t)elem(d->dtype), a = reinterpret_cast<uintptr_t>(d_x), b = reinterpret_cast<uintptr_t>(other);
+  return a < b + (uintptr_t)((d->rows - 1) * stride + d->d) * e && b < a + (uintptr_t)((d->rows - 1) * d->out_stride + d->d) * e;
+}
 bool rows_apart(const layer_norm_desc* d, int64_t stride) { return d->rows < 2 || stride >= d->d; }
 
 // ---- AdamW
@@ -193,6 +198,7 @@ extern "C" int rope_readout_axes(const seco_desc* desc, const rope_axes* axes, c
 
 extern "C" size_t layer_norm_workspace_bytes(const layer_norm_desc* desc) {
   if (check_norm(desc)) return (size_t)-1;
+  if (norm_few(desc->rows, desc->d, desc->dtype)) return 0;
   return (size_t)2 * norm_blocks(desc->rows, desc->d, desc->dtype) * desc->d * sizeof(float);
 }
 
@@ -231,7 +237,8 @@ extern "C" int layer_norm_bwd(const layer_norm_desc* desc, const void* x, const 
   if (!aligned(gain, ge) || !aligned(d_gain, ge) || !aligned(d_bias, ge) || !aligned(mean, 4) || !aligned(rstd, 4)) return SECO_ERR_ALIGN;
   if (!rows_apart(desc, desc->out_stride)) return SECO_ERR_SHAPE;
   const bool sums = d_gain || d_bias;
-  if (sums && (!ws || !aligned(ws, 16) || ws_bytes < layer_norm_workspace_bytes(desc))) return SECO_ERR_WORKSPACE;
+  const bool few = sums && norm_few(desc->rows, desc->d, desc->dtype);
+  if (sums && !few && (!ws || !aligned(ws, 16) || ws_bytes < layer_norm_workspace_bytes(desc))) return SECO_ERR_WORKSPACE;
   if (desc->rows == 0 && !sums) return SECO_OK;
   NormArgs a = norm_args(desc);
   a.x = x;
@@ -241,9 +248,16 @@ extern "C" int layer_norm_bwd(const layer_norm_desc* desc, const void* x, const 
   a.rstd = const_cast<float*>(rstd);
   a.dy = d_y;
   a.out = d_x;
-  a.parts = sums ? static_cast<float*>(ws) : nullptr;
   a.blocks = a.part_rows = norm_blocks(desc->rows, desc->d, desc->dtype);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (few) {                                     // (d_x in the place of what the sums are made of: the sums first)
+    a.d_gain = d_gain;
+    a.d_bias = d_bias;
+    const bool apart = !overlap(desc, d_x, x, desc->x_stride) && !overlap(desc, d_x, d_y, desc->y_stride);
+    rc = launch_norm_bwd_few(a, apart, s);
+    return rc || apart ? rc : launch_norm_bwd(a, s);
+  }
+  a.parts = sums ? static_cast<float*>(ws) : nullptr;
   rc = launch_norm_bwd(a, s);
   if (rc || !sums) return rc;
   return launch_norm_sums(a.parts, a.blocks, a.d, d_gain, d_bias, a.gain_f32, s);

@@ -145,7 +145,7 @@ PyObject* norm_bwd(PyObject* const* a) {
   if (with_gain || with_bias) {
     const size_t n = lib.layer_norm_workspace_bytes(&d);
     if (n == (size_t)-1) check(SECO_ERR_SHAPE, "layer_norm_workspace_bytes");
-    ws = ws_given ? *ws_given : scratch((int64_t)n, x, on.s);
+    if (n > 0) ws = ws_given ? *ws_given : scratch((int64_t)n, x, on.s);
   }
   // (an empty tensor has no address; nothing is read or written there)
   void* some = with_gain ? ptr(dg) : with_bias ? ptr(db) : nullptr;

@@ -117,6 +117,31 @@ def test_backward(t, d, rows, d_in):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,d", [(1, 3), (2, 1024), (129, 45), (513, 260), (1024, 1027), (1025, 1027), (300, 16384), (40, 16390)])
+def test_where_the_results_lie_changes_nothing(t, rows, d):
+    """d_x apart, in the place of x, of d_y or (one row apart in the same buffer) beside x: the same bits; one sum without the other."""
+    dtype = TYPES[t]
+    x, dy = _on_gpu(_rows(60, rows, d, dtype)), _on_gpu(_rows(61, rows, d, dtype))
+    gain = _rows(62, 1, d, dtype)[0].contiguous().to(DEV)
+    _, mean, rstd = seco.layer_norm_fwd(x, gain)
+    first = seco.layer_norm_bwd(x, gain, mean, rstd, dy)
+    for place in ("x", "d_y"):
+        x2, dy2 = x.clone(), dy.clone()
+        got = seco.layer_norm_bwd(x2, gain, mean, rstd, dy2, d_x=x2 if place == "x" else dy2)
+        assert got[0] is (x2 if place == "x" else dy2)
+        assert all(torch.equal(a, b) for a, b in zip(got, first)), place
+    wide = torch.empty(rows, 2 * d, dtype=dtype, device=DEV)
+    wide[:, :d] = x
+    got = seco.layer_norm_bwd(wide[:, :d], gain, mean, rstd, dy, d_x=wide[:, d:])
+    assert all(torch.equal(a, b) for a, b in zip(got, first)) and torch.equal(wide[:, :d], x)
+    only = seco.layer_norm_bwd(x, gain, mean, rstd, dy, with_bias=False)
+    assert only[2] is None and torch.equal(only[1], first[1]) and torch.equal(only[0], first[0])
+    only = seco.layer_norm_bwd(x, gain, mean, rstd, dy, with_gain=False)
+    assert only[1] is None and torch.equal(only[2], first[2]) and torch.equal(only[0], first[0])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("t,d", [("bf16", 1024), ("bf16", 4096), ("bf16", 130), ("bf16", 20001), ("f32", 8192), ("f32", 63)])
 def test_results_are_the_same_every_time(t, d):
     dtype = TYPES[t]
@@ -401,9 +426,12 @@ def test_status_codes():
     assert fwd(desc(d=(1 << 30) + 1)) == -10 and fwd(desc(rows=(1 << 31) + 1)) == -10
     assert fwd(desc(), x=C.c_void_p(0x1001)) == -5 and fwd(desc(), mean=C.c_void_p(0x1002)) == -5
     assert fwd(desc(rows=0)) == 0                                   # nothing to do
-    assert bwd(desc(), ws=None) == -6 and bwd(desc(), n=16) == -6 and bwd(desc(), ws=C.c_void_p(0x1008)) == -6
+    many = desc(rows=2000)                                          # (few rows take no workspace; these addresses are never read)
+    assert bwd(many, ws=None) == -6 and bwd(many, n=16) == -6 and bwd(many, ws=C.c_void_p(0x1008)) == -6
     assert bwd(desc(), dx=None) == -1 and bwd(desc(), dg=C.c_void_p(0x1001)) == -5
     lib.layer_norm_workspace_bytes.restype = C.c_size_t
-    assert lib.layer_norm_workspace_bytes(C.byref(desc())) == 2 * 16 * 4
+    assert lib.layer_norm_workspace_bytes(C.byref(desc())) == 0 and lib.layer_norm_workspace_bytes(C.byref(desc(rows=1024))) == 0
+    assert lib.layer_norm_workspace_bytes(C.byref(desc(rows=0))) == 2 * 16 * 4
+    assert lib.layer_norm_workspace_bytes(C.byref(desc(rows=1025))) > 0 and lib.layer_norm_workspace_bytes(C.byref(desc(d=16385))) > 0
     assert lib.layer_norm_workspace_bytes(C.byref(desc(rows=100000))) == 2 * 256 * 16 * 4
     assert lib.layer_norm_workspace_bytes(C.byref(desc(d=-1))) == C.c_size_t(-1).value
