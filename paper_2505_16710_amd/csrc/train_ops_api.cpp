@@ -1,6 +1,7 @@
 // Entry points of the operators around the training step: argument checks, and what the launchers need.  Host code only;
 // nothing here allocates device memory, synchronises or keeps state between calls.
 #include <cmath>
+#include <initializer_list>
 
 #include "decoder.h"
 #include "train_ops.h"
@@ -130,8 +131,9 @@ int set_part(RopePart& p, const seco_desc* d, const void* in, void* out, int hea
   if (heads < 1) return SECO_ERR_SHAPE;
   if (heads > 65535) return SECO_ERR_TOO_LARGE;
   for (int i = 0; i < 3; ++i) {
+    const int64_t most = (int64_t)1 << (i == 2 ? 30 : 40);          // (rows start at row * stride, row up to 2^30)
+    if (is[i] > most || os[i] > most) return SECO_ERR_TOO_LARGE;
     if (is[i] < 0 || is[i] * in_elem % 16 || os[i] < 0 || os[i] * out_elem % 16) return SECO_ERR_ALIGN;
-    if (is[i] > (int64_t)1 << 40 || os[i] > (int64_t)1 << 40) return SECO_ERR_TOO_LARGE;
   }
   if (is[2] < d->head_dim || os[2] < d->head_dim) return SECO_ERR_ALIGN;
   if (!aligned(in, 16) || !aligned(out, 16)) return SECO_ERR_ALIGN;
