@@ -116,6 +116,11 @@ template <typename T, int V> struct Pack {
     for (int i = 0; i < kWords; ++i) x.w[i] = w[i] & m;
     return x;
   }
+  // The load of this word has returned here
+  __device__ __forceinline__ void arrived() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) asm volatile("" : "+v"(w[i]));
+  }
   // What is computed from the elements behind this point waits for `after`, and is not what was computed from them in front of
   // it: the compiler would keep the fp32 values of several rows in registers instead of their half as large words.
   __device__ __forceinline__ void renew(float after) {

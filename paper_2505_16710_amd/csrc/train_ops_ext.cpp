@@ -17,6 +17,15 @@ struct OnGpu {
   void* s;
   OnGpu(const Tensor& t, PyObject* o) : guard(t.device()), s(o == Py_None ? c10::hip::getCurrentHIPStream(t.device().index()).stream() : stream(o)) {}
 };
+// a result in the place of an input lies there element for element
+void in_place_or_apart(const Tensor& out, const Tensor& in, const char* name) {
+  if (out.data_ptr() != in.data_ptr() || out.numel() == 0) return;
+  for (int64_t i = 0; i < in.dim(); ++i)
+    if (in.size(i) > 1 && out.stride(i) != in.stride(i)) {
+      PyErr_Format(PyExc_ValueError, "%s: in the place of an input it needs that one's strides", name);
+      throw Raised{};
+    }
+}
 void same_gpu(const Tensor& a, const Tensor& b) {
   if (!a.is_cuda() || a.device() != b.device()) raise(PyExc_ValueError, "the tensors must be on one GPU");
 }
@@ -95,12 +104,16 @@ PyObject* norm_fwd(PyObject* const* a) {
   if (bias) vector_of(*bias, rows.d, gt, "bias");
   if (res) d.residual_stride = rows_like(*res, x, "residual").stride;
   else if (a[6] != Py_None) raise(PyExc_ValueError, "x_out goes with a residual");
-  for (const Tensor* t : {gain, bias, res})
-    if (t) same_gpu(x, *t);
   const Tensor *y_given = opt_tensor(a[5]), *out_given = opt_tensor(a[6]);
   for (const Tensor* t : {y_given, out_given})
-    if (t) rows_like(*t, x, t == y_given ? "y" : "x_out"), same_gpu(x, *t);
-  same_gpu(x, x);
+    if (t) {
+      const char* name = t == y_given ? "y" : "x_out";
+      rows_like(*t, x, name);
+      in_place_or_apart(*t, x, name);
+      if (res) in_place_or_apart(*t, *res, name);
+    }
+  for (const Tensor* t : {&x, gain, bias, res, y_given, out_given})
+    if (t) same_gpu(x, *t);
   OnGpu on(x, a[7]);
   const Tensor y = given_or(a[5], x);
   Tensor out;
@@ -130,7 +143,11 @@ PyObject* norm_bwd(PyObject* const* a) {
       raise(PyExc_ValueError, "mean, rstd: contiguous float32, one value per row");
   d.y_stride = rows_like(dy, x, "d_y").stride;
   if (in) d.residual_stride = rows_like(*in, x, "d_in").stride;
-  if (dx_given) rows_like(*dx_given, x, "d_x");
+  if (dx_given) {
+    rows_like(*dx_given, x, "d_x");
+    for (const Tensor* t : {&x, &dy, in})
+      if (t) in_place_or_apart(*dx_given, *t, "d_x");
+  }
   for (const Tensor* t : {&mean, &rstd, &dy, gain, in, dx_given, ws_given})
     if (t) same_gpu(x, *t);
   const int with_gain = PyObject_IsTrue(a[7]), with_bias = PyObject_IsTrue(a[8]);
@@ -219,7 +236,10 @@ PyObject* adamw(PyObject* const* a) {
   d.state_bits = eight ? 8 : 32;
   const auto list = std::make_unique<adamw_tensor[]>((size_t)n);
   std::vector<std::pair<uintptr_t, uintptr_t>> places;
-  places.reserve((size_t)n);
+  places.reserve((size_t)n * 6);
+  auto written = [&](const Tensor& x) {
+    if (x.numel() > 0) places.emplace_back((uintptr_t)ptr(x), (uintptr_t)ptr(x) + nbytes(x));
+  };
   for (Py_ssize_t i = 0; i < n; ++i) {
     const Tensor &p = params[i], &g = grads[i], &m = ms[i], &v = vs[i];
     adamw_tensor& t = list[i];
@@ -248,18 +268,23 @@ PyObject* adamw(PyObject* const* a) {
           bad(PyExc_ValueError, "m_scales, v_scales", i, "one contiguous float32 per 256 elements of the parameter");
       t.m_scale = fptr(m_scales[i]);
       t.v_scale = fptr(v_scales[i]);
+      written(m_scales[i]);
+      written(v_scales[i]);
     }
     if (masters.s && masters.item(i) != Py_None) {
       const Tensor& w = masters[i];
       if (w.scalar_type() != at::kFloat || p.scalar_type() != at::kBFloat16) bad(PyExc_TypeError, "masters", i, "float32, of bfloat16 parameters only");
       same_places(w, p, "masters", i);
       t.master = fptr(w);
+      written(w);
     }
-    if (t.n > 0) places.emplace_back((uintptr_t)t.param, (uintptr_t)t.param + nbytes(p));
+    written(p);
+    written(m);
+    written(v);
   }
   std::sort(places.begin(), places.end());
   for (size_t i = 1; i < places.size(); ++i)
-    if (places[i].first < places[i - 1].second) raise(PyExc_ValueError, "params: two of them overlap, or one is there twice");
+    if (places[i].first < places[i - 1].second) raise(PyExc_ValueError, "params and their states: two of them overlap, or one is there twice");
   if (!step.is_cuda()) raise(PyExc_ValueError, "the tensors must be on one GPU");
   OnGpu on(step, a[14]);
   check(lib.adamw_step(&d, list.get(), (int32_t)n, static_cast<int64_t*>(ptr(step)), on.s), "adamw_step");
@@ -305,7 +330,7 @@ void like_each_other(const Tensor& a, const Tensor& b, const char* names) {
 // rows [begin, begin + n) of a cache or gradient buffer [B, H, N, D]
 void rows_inside(const Tensor& t, const char* name, int64_t B, int64_t H, int64_t D, int64_t begin, int64_t n, at::ScalarType type) {
   if (t.dim() == 4 && t.size(0) == B && t.size(1) == H && t.size(3) == D && t.stride(3) == 1 && t.scalar_type() == type && begin >= 0 &&
-      begin + n <= t.size(2))
+      begin <= t.size(2) - n)
     return;
   PyErr_Format(PyExc_ValueError, "%s: expected [%lld, %lld, rows, %lld] with contiguous head_dim that holds rows %lld to %lld", name,
                (long long)B, (long long)H, (long long)D, (long long)begin, (long long)(begin + n));
@@ -360,6 +385,7 @@ PyObject* rotate_axes(PyObject* const* a) {
     heads_tensor(o, "out", B, C, D, x.scalar_type());
     writable(o, "out");
     if (o.size(1) != x.size(1)) raise(PyExc_ValueError, "out must have the shape of x");
+    in_place_or_apart(o, x, "out");
     same_gpu(x, o);
   }
   same_gpu(x, pos);
@@ -383,6 +409,7 @@ PyObject* append_axes(PyObject* const* a) {
   if (kn.dim() != 4) raise(PyExc_ValueError, "k_new: expected a [batch, head, row, head_dim] tensor");
   const int64_t B = kn.size(0), Hkv = kn.size(1), C = kn.size(2), D = kn.size(3);
   heads_tensor(kn, "k_new", B, C, D, kn.scalar_type());
+  if (Hkv < 1) raise(PyExc_ValueError, "k_new: expected at least one head");
   fits_axes(axes, D);
   like_each_other(kn, vn, "k_new and v_new");
   like_each_other(kc, vc, "k_cache and v_cache");
@@ -397,6 +424,7 @@ PyObject* append_axes(PyObject* const* a) {
     heads_tensor(o, "q_out", B, C, D, kn.scalar_type());
     writable(o, "q_out");
     if (!q || o.size(1) != q->size(1)) raise(PyExc_ValueError, "q_out must have the shape of q");
+    in_place_or_apart(o, *q, "q_out");
     same_gpu(kn, o);
   }
   for (const Tensor* t : {&vn, &kc, &vc, &pos, q})
@@ -438,6 +466,7 @@ PyObject* readout_axes(PyObject* const* a) {
   }
   if (type != at::kBFloat16 && type != at::kFloat) raise(PyExc_TypeError, "unsupported dtype: expected bfloat16 or float32");
   like_each_other(gk, gv, "gk and gv");
+  if (Hkv < 1) raise(PyExc_ValueError, "gk: expected at least one head");
   rows_inside(gk, "gk", B, Hkv, D, row, C, at::kFloat);
   fits_axes(axes, D);
   if (dq) heads_tensor(*dq, "d_q", B, C, D, type);
@@ -456,6 +485,7 @@ PyObject* readout_axes(PyObject* const* a) {
     heads_tensor(o, "dq_out", B, C, D, type);
     writable(o, "dq_out");
     if (!dq || o.size(1) != dq->size(1)) raise(PyExc_ValueError, "dq_out must have the shape of d_q");
+    in_place_or_apart(o, *dq, "dq_out");
     same_gpu(gk, o);
   }
   for (const Tensor* t : {&gv, &pos, dq, dk_given, dv_given})

@@ -395,6 +395,11 @@ def test_refusals():
                dict(p=[x, x], g=[x, x], m=[x, x], v=[x, x]), dict(p=[x, x[5:]], g=[x, x[5:]], m=[x, x[5:]], v=[x, x[5:]])):
         with pytest.raises(ValueError):
             call(**kw)
+    y, w = torch.zeros(300), torch.zeros(600)
+    for kw in (dict(p=[y], m=[x], v=[x]), dict(p=[y], m=[y], v=[x]), dict(p=[half], m=[w[:300]], v=[x], masters=[w[299:599]]),
+               dict(p=[y], m=[f8], v=[f8.clone()], m_scales=u, v_scales=u)):
+        with pytest.raises(ValueError, match="overlap"):
+            call(**kw)
     for kw in (dict(p=[x.half()]), dict(g=[x.double()]), dict(m=[half]), dict(m=[f8], v=[f8]), dict(m_scales=u, v_scales=u),
                dict(masters=[x]), dict(p=[half], masters=[half]), dict(p=[1.0]), dict(lr="fast")):
         with pytest.raises(TypeError):

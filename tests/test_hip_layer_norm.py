@@ -142,6 +142,19 @@ def test_where_the_results_lie_changes_nothing(t, rows, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t,rows,d", [("bf16", 700, 4099), ("bf16", 2500, 4099), ("bf16", 1100, 12001), ("f32", 300, 4102), ("f32", 3000, 2051)])
+def test_gradient_added_in_place(t, rows, d):
+    """d_x in the place of d_in, rows whose last words overlap across wavefronts: the same bits as apart."""
+    dtype = TYPES[t]
+    x, dy, extra = (_on_gpu(_rows(63 + i, rows, d, dtype)) for i in range(3))
+    _, mean, rstd = seco.layer_norm_fwd(x, None)
+    apart = seco.layer_norm_bwd(x, None, mean, rstd, dy, d_in=extra)
+    place = extra.clone()
+    got = seco.layer_norm_bwd(x, None, mean, rstd, dy, d_in=place, d_x=place)
+    assert got[0] is place and all(torch.equal(a, b) for a, b in zip(got, apart))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("t,d", [("bf16", 1024), ("bf16", 4096), ("bf16", 130), ("bf16", 20001), ("f32", 8192), ("f32", 63)])
 def test_results_are_the_same_every_time(t, d):
     dtype = TYPES[t]
@@ -385,6 +398,13 @@ def test_refusals():
         fwd(x, residual=x.bfloat16())
     with pytest.raises(ValueError, match="x_out"):
         fwd(x, x_out=x)
+    wide = torch.zeros(256)
+    there, other = wide.view(8, 32)[:4, :16], wide.view(4, 64)[:, :16]      # rows from one place on, at two distances
+    for kw in (dict(y=other), dict(residual=there, x_out=other)):
+        with pytest.raises(ValueError, match="strides"):
+            fwd(there, **kw)
+    with pytest.raises(ValueError, match="strides"):
+        bwd(there, None, torch.zeros(4), torch.zeros(4), x, d_x=other)
     with pytest.raises(ValueError, match="mean"):
         bwd(x, g, m[:3], m, x)
     with pytest.raises(ValueError, match="mean"):

@@ -104,6 +104,30 @@ def test_layer_norms_without_biases_and_one_gain_for_all_columns():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layers", [0, 1])
+def test_few_layers(layers, monkeypatch):
+    for sizes in (F32, BF16):
+        monkeypatch.setitem(sizes, "n_layers", layers)
+    for dtype, tol in ((torch.float32, 5e-4), (torch.bfloat16, 6e-2)):
+        cfg, p64, params, dec, tok, tgt, pos = _setup(21, 2, 96, dtype, **_options("both", dtype))
+        _, ref = om.monolithic_grads(cfg, p64, tok, tgt, pos)
+        _, got = dec.step(tok.to(DEV), tgt.to(DEV), 32, positions=pos.to(DEV))
+        _compare(ref, got, tol)
+
+
+@pytest.mark.gpu
+def test_an_fp32_tail_behind_a_bf16_body():
+    """Final norm (its bias too) and head in fp32: the logits are fp32."""
+    cfg, p64, params, dec, tok, tgt, pos = _setup(23, 1, 128, torch.bfloat16, **_options("both", torch.bfloat16))
+    for n in ("norm_f", "norm_f_b", "head"):
+        params[n] = params[n].detach().float().requires_grad_()
+    _, ref = om.monolithic_grads(cfg, p64, tok, tgt, pos)
+    _, got = dec.step(tok.to(DEV), tgt.to(DEV), 64, positions=pos.to(DEV))
+    assert all(got[n].dtype == torch.float32 for n in ("norm_f", "norm_f_b", "head"))
+    _compare(ref, got, 6e-2)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_text_positions_are_those_of_one_axis(dtype):
     """Without positions every axis counts the tokens: the step of rope_base, to rounding."""

@@ -302,6 +302,20 @@ def test_refusals():
     for bad in (x[0], x[..., :120], torch.zeros(1, 2, 128, 10).transpose(2, 3)):
         with pytest.raises(ValueError):
             rot(bad)
+    with pytest.raises(ValueError, match="strides"):
+        rot(x, out=x.view(1, 10, 2, 128).transpose(1, 2))          # in the place of x, its rows in another order
+    with pytest.raises(ValueError, match="strides"):
+        app(q_out=x.view(1, 10, 2, 128).transpose(1, 2))
+    with pytest.raises(ValueError, match="strides"):
+        rea(dq_out=x.view(1, 10, 2, 128).transpose(1, 2))
+    with pytest.raises(ValueError, match="at least one head"):
+        app(k=x[:, :0], v=x[:, :0], kc=c[:, :0], vc=c[:, :0])
+    with pytest.raises(ValueError, match="at least one head"):
+        rea(gk=g[:, :0], gv=g[:, :0])
+    for row in (-1, 41, 2 ** 63 - 1, 2 ** 63 - 5):
+        for call in (app, rea):
+            with pytest.raises(ValueError, match="holds rows"):
+                call(row=row)
     for bad in (pos[:1], pos[..., :9], pos.int(), pos[0], torch.zeros(2, 3, 10, dtype=torch.int64)):
         for call in (rot, app):
             with pytest.raises(ValueError):
