@@ -328,12 +328,13 @@ template <typename T, int V, int KB> struct Columns {
   }
 };
 
-// G <= 64 lanes to a row: no barrier in the loop.  At the end the groups' sums meet in LDS and leave as the workgroup's row of
-// the parts, in the order of the wavefronts.
+// G <= 64 lanes to a row: no barrier in the loop.  At the end the groups' sums meet in LDS, behind one barrier, and leave as the
+// workgroup's row of the parts, in the order of the wavefronts.  The last row is taken behind the loop, so that nothing is
+// requested that is not there (with both: 2048 x 1024 bf16 10.0 -> 9.0 us, its sums included).
 template <typename T, int V, int G, int KB, bool IN>
 __global__ __launch_bounds__(kBlock) void norm_bwd_rows_kernel(NormArgs a) {
-  constexpr int kRows = kBlock / G, kWaves = kBlock / 64, kCols = G * KB * V;
-  __shared__ float sh[kWaves][kCols];
+  constexpr int kRows = kBlock / G, kWaves = kBlock / 64, kCols = G * KB * V, kOwn = (kCols + kBlock - 1) / kBlock;
+  __shared__ float sh[2][kWaves][kCols];
   const int lane = threadIdx.x % G, wave = threadIdx.x >> 6, d = (int)a.d;
   const float inv = 1.f / (float)d;
   const Words<T, V, G, KB> at(lane, d);
@@ -341,9 +342,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_rows_kernel(NormArgs a) {
   int64_t row = row_of<G>((int64_t)blockIdx.x * kRows + threadIdx.x / G);
   const int64_t step = (int64_t)a.blocks * kRows;
   Held<T, V, KB, 1, IN, false> now, next;
-  if (row < a.rows) now.load(a, row, 1, at);
-  for (; row < a.rows; row += step) {
-    next.load(a, row + step < a.rows ? row + step : row, 1, at);
+  auto take_row = [&]() {
     float s1, s2;
     c.add(now.x[0], now.y[0], 0xffffffffu, now.mean[0], now.rstd[0], s1, s2);
     c.settle();
@@ -364,33 +363,53 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_rows_kernel(NormArgs a) {
       }
       if (at[k].skip < V) Pack<T, V>::of(f).to(out, at[k].at);
     }
-    now = next;
+  };
+  if (row < a.rows) {
+    now.load(a, row, 1, at);
+    for (; row + step < a.rows; row += step) {
+      next.load(a, row + step, 1, at);
+      take_row();
+      now = next;
+    }
+    take_row();
   }
   if (!a.parts) return;
-  auto leave = [&](float (&s)[KB][V], float* part) {
+  float old[2][kOwn];                             // of this thread's columns, under the sums over the wavefronts
+  float* part[2] = {a.parts + (int64_t)blockIdx.x * d, a.parts + ((int64_t)a.part_rows + blockIdx.x) * d};
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+      const int i = k * kBlock + threadIdx.x;
+      old[q][k] = a.accumulate ? part[q][min(i, d - 1)] : 0.f;
+    }
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    auto& s = q ? c.db : c.dg;
     if constexpr (G == 16)
 #pragma unroll
       for (int k = 0; k < KB; ++k)
 #pragma unroll
         for (int j = 0; j < V; ++j) s[k][j] = sum_across_32(sum_across_16(s[k][j]));
-    __syncthreads();
     if ((threadIdx.x & 63) < G)
 #pragma unroll
       for (int k = 0; k < KB; ++k)
 #pragma unroll
         for (int j = 0; j < V; ++j)
-          if (j >= at[k].skip) sh[wave][at[k].at + j] = s[k][j];
-    __syncthreads();
-    for (int i = threadIdx.x; i < d; i += kBlock) {
-      float f = sh[0][i];
+          if (j >= at[k].skip) sh[q][wave][at[k].at + j] = s[k][j];
+  }
+  __syncthreads();
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) f += sh[w][i];
-      part[i] = (a.accumulate ? part[i] : 0.f) + f;
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+      const int i = k * kBlock + threadIdx.x;
+      if (i >= d) break;
+      float f = sh[q][0][i];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) f += sh[q][w][i];
+      part[q][i] = old[q][k] + f;
     }
-  };
-  float* part = a.parts + (int64_t)blockIdx.x * d;
-  leave(c.dg, part);
-  leave(c.db, part + (int64_t)a.part_rows * d);
 }
 
 // A workgroup to a row, R rows at a time: one barrier for their 2 R sums.  AHEAD: the next rows are requested under the present
@@ -601,7 +620,8 @@ template <typename T, int V> __device__ __forceinline__ void column_sums(const N
   float f = sh[0][l][k][j];
 #pragma unroll
   for (int w = 1; w < kBlock / 64; ++w) f += sh[w][l][k][j];
-  if (sizeof(T) == 4 || a.gain_f32) static_cast<float*>(out)[to.at + j] = f;
+  if (a.accumulate) static_cast<float*>(out)[to.at + j] += f;
+  else if (sizeof(T) == 4 || a.gain_f32) static_cast<float*>(out)[to.at + j] = f;
   else static_cast<T*>(out)[to.at + j] = (T)f;
 }
 template <typename T, int V, int G, int KB, bool IN>
@@ -754,8 +774,8 @@ template <typename T> int norm_bwd_few(NormArgs a, bool rows_too, hipStream_t s)
 
 // Up to 1024 rows (beyond, the walk down the rows is the longest way: 2048 x 45 bf16 10.5 us, by parts 7.0), while x and d_y are
 // held by the caches between the two readings: up to 16 MiB each.  us on the GPU, one launch / parts and their sums: bf16
-// 16 x 1024 3.4 / 8.3, 512 x 4096 6.1 / 14.2, 1024 x 8192 18.4 / 26.8; fp32 1024 x 4096 15.2 / 16.6, but 1024 x 8192 26.3 / 27.7 and
-// 2048 x 4096 30.5 / 23.5.
+// 16 x 1024 3.6 / 7.5, 512 x 4096 6.2 / 14.2, 1024 x 8192 18.0 / 27.0, but 1024 x 45 6.7 / 6.1 (in wall time 6.7 / 8.9); fp32 1024 x 4096
+// 14.7 / 17.0, 1024 x 8192 (not taken) 27.8 / 28.1, 2048 x 4096 (not taken) 30.5 / 23.5.
 bool norm_few(int64_t rows, int64_t d, int dtype) {
   const int64_t elem = dtype == SECO_BF16 ? 2 : 4;
   return rows >= 1 && rows <= 1024 && d * elem <= 32768 && rows * d * elem <= (int64_t)16 << 20;   // (32768: backward_shape's longest)

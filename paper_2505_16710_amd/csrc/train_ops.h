@@ -23,7 +23,7 @@ struct NormArgs {
   int64_t rows, d, xs, rs, os, ys;
   float eps;
   int dtype, gain_f32;           // gain_f32: gain and bias are fp32 (else of dtype)
-  void *d_gain, *d_bias;         // backward of few rows: the sums themselves (either NULL)
+  void *d_gain, *d_bias;         // backward of few rows: the sums themselves (either NULL), fp32 with accumulate
   int blocks, accumulate;        // workgroups that leave sums; 1: they are added to what is there
   // forward, first norm of a decoder: row r of x is row token[r] of a table of `table` rows
   const int64_t* token;

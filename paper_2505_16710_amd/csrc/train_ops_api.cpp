@@ -370,9 +370,14 @@ extern "C" int dec_layer_norm_bwd(int dtype, const void* x, const void* gain, co
   a.out = d_x;
   a.mean = const_cast<float*>(mean);
   a.rstd = const_cast<float*>(rstd);
-  a.parts = parts;
   a.part_rows = SECO_NORM_BLOCKS;
-  a.blocks = norm_blocks(rows, d, dtype);
   a.accumulate = 1;
+  if (norm_few(rows, d, dtype)) {                // (into the first share; d_x overwrites neither x nor d_h here)
+    a.d_gain = parts;
+    a.d_bias = parts + SECO_NORM_BLOCKS * d;
+    return launch_norm_bwd_few(a, true, static_cast<hipStream_t>(stream));
+  }
+  a.parts = parts;
+  a.blocks = norm_blocks(rows, d, dtype);
   return launch_norm_bwd(a, static_cast<hipStream_t>(stream));
 }
