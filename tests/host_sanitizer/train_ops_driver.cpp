@@ -92,7 +92,9 @@ static void layer_norms() {
   CHECK(dec_layer_norm_bwd(SECO_BF16, at(0x100), at(0x200), m, r, at(0x300), at(0x400), at(0x400), at<float>(0x1000), 0, 9, nullptr) == SECO_OK &&
         log_.bwd.empty());
   CHECK(dec_layer_norm_bwd(SECO_BF16, at(0x100), at(0x200), m, r, at(0x300), at(0x400), at(0x400), at<float>(0x1000), 3, 9, nullptr) == SECO_OK);
-  CHECK(log_.bwd.size() == 1 && log_.bwd[0].accumulate == 1 && log_.bwd[0].part_rows == SECO_NORM_BLOCKS && log_.bwd[0].blocks == 3);
+  CHECK(log_.few.size() == 1 && log_.few[0].accumulate == 1 && log_.few[0].d_bias == at(0x1000 + SECO_NORM_BLOCKS * 9 * 4) && log_.bwd.empty());
+  CHECK(dec_layer_norm_bwd(SECO_BF16, at(0x100), at(0x200), m, r, at(0x300), at(0x400), at(0x400), at<float>(0x1000), 3000, 9, nullptr) == SECO_OK);
+  CHECK(log_.bwd.size() == 1 && log_.bwd[0].accumulate == 1 && log_.bwd[0].part_rows == SECO_NORM_BLOCKS && log_.bwd[0].blocks == SECO_NORM_BLOCKS);
 }
 
 static adamw_tensor tensor(int64_t n, int param, int grad, bool master) {
