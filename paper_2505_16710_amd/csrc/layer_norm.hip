@@ -185,10 +185,31 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_kernel(NormArgs a)
   }
 }
 
-// Rows longer than a workgroup's registers: three walks over the row (the second and third from the caches).
+// Rows longer than a workgroup's registers are walked over by words of V elements, U at a time: f(V, places, whether they are
+// there); what is left behind the last whole word, by single elements.  A place is always the same thread's, so that a result
+// may lie over what it is made of.
+template <int V, int U, typename F> __device__ __forceinline__ void walk(int64_t d, F f) {
+  const unsigned words = (unsigned)(d / V);
+  for (unsigned w = threadIdx.x; w < words; w += U * kBlock) {
+    unsigned at[U];
+    bool there[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      there[u] = w + u * kBlock < words;
+      at[u] = (there[u] ? w + u * kBlock : w) * V;
+    }
+    f(std::integral_constant<int, V>{}, at, there);
+  }
+  unsigned at[1] = {words * V + threadIdx.x};
+  bool there[1] = {true};
+  if (at[0] < d) f(std::integral_constant<int, 1>{}, at, there);
+}
+
+// Three walks over the row (the second and third from the caches): 4096 x 16384 fp32 with a residual 238 us, by single elements 370.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void norm_fwd_long_kernel(NormArgs a) {
   __shared__ float sh[2][kBlock / 64][2];
+  constexpr int kV = 16 / sizeof(T), kU = 4;
   const int64_t row = (int64_t)blockIdx.y * kGridX + blockIdx.x, d = a.d;
   if (row >= a.rows) return;
   const T* x = static_cast<const T*>(a.x) + row * a.xs;
@@ -202,24 +223,50 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_long_kernel(NormArgs a) {
     x = static_cast<const T*>(a.x) + (bad ? 0 : t) * a.xs;
   }
   T* out = a.out ? static_cast<T*>(a.out) + row * a.os : nullptr;
-  // out may lie over x or r: an element is read and written by one thread, and read again from out
-  auto first = [&](int64_t c) {
-    float f = bad ? NAN : (float)x[c];
-    if (r) f = (float)(T)(f + (float)r[c]);
-    if (out) out[c] = (T)f;
-    return f;
-  };
-  auto again = [&](int64_t c) { return out ? (float)out[c] : bad ? NAN : (float)x[c]; };
+  const T* s = out ? out : x;                    // the row that is normalised, from the second walk on
   float sum[1] = {0.f};
-  for (int64_t c = threadIdx.x; c < d; c += kBlock) sum[0] += first(c);
+  walk<kV, kU>(d, [&](auto v, auto& at, auto& there) {
+    constexpr int V = decltype(v)::value, U = std::extent<std::remove_reference_t<decltype(at)>>::value;
+    Pack<T, V> w[U], rw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      w[u] = Pack<T, V>::at(x, at[u]);
+      if (r) rw[u] = Pack<T, V>::at(r, at[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float f[V], g[V];
+      w[u].get(f);
+      if (r) rw[u].get(g);
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] = bad ? NAN : r ? f[j] + g[j] : f[j];
+      const Pack<T, V> rounded = Pack<T, V>::of(f);
+      rounded.get(f);
+      if (out && there[u]) rounded.to(out, at[u]);
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[0] += there[u] ? f[j] : 0.f;
+    }
+  });
   block_sums<kBlock, 1>(sum, reinterpret_cast<float(*)[1]>(sh[0]));
   const float inv = 1.f / (float)d, m0 = sum[0] * inv;
   float two[2] = {0.f, 0.f};
-  for (int64_t c = threadIdx.x; c < d; c += kBlock) {
-    const float dev = again(c) - m0;
-    two[0] += dev;
-    two[1] += dev * dev;
-  }
+  walk<kV, kU>(d, [&](auto v, auto& at, auto& there) {
+    constexpr int V = decltype(v)::value, U = std::extent<std::remove_reference_t<decltype(at)>>::value;
+    Pack<T, V> w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = Pack<T, V>::at(s, at[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float f[V];
+      w[u].get(f);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float dev = there[u] ? f[j] - m0 : 0.f;
+        two[0] += dev;
+        two[1] += dev * dev;
+      }
+    }
+  });
   block_sums<kBlock, 2>(two, sh[1]);
   const float delta = two[0] * inv, var = fmaxf(two[1] * inv - delta * delta, 0.f), rstd = 1.f / sqrtf(var + a.eps);
   if (threadIdx.x == 0) {
@@ -227,18 +274,30 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_long_kernel(NormArgs a) {
     a.rstd[row] = rstd;
   }
   T* y = static_cast<T*>(a.y) + row * a.ys;
-  for (int64_t c = threadIdx.x; c < d; c += kBlock) {
-    float f = ((again(c) - m0) - delta) * rstd, g[1];
-    if (a.gain) {
-      load_gain<T, 1>(a.gain, a.gain_f32, (unsigned)c, g);
-      f *= g[0];
+  walk<kV, kU>(d, [&](auto v, auto& at, auto& there) {
+    constexpr int V = decltype(v)::value, U = std::extent<std::remove_reference_t<decltype(at)>>::value;
+    Pack<T, V> w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = Pack<T, V>::at(s, at[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float f[V], g[V];
+      w[u].get(f);
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] = ((f[j] - m0) - delta) * rstd;
+      if (a.gain) {
+        load_gain<T, V>(a.gain, a.gain_f32, at[u], g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] *= g[j];
+      }
+      if (a.bias) {
+        load_gain<T, V>(a.bias, a.gain_f32, at[u], g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] += g[j];
+      }
+      if (there[u]) Pack<T, V>::of(f).to(y, at[u]);
     }
-    if (a.bias) {
-      load_gain<T, 1>(a.bias, a.gain_f32, (unsigned)c, g);
-      f += g[0];
-    }
-    y[c] = (T)f;
-  }
+  });
 }
 
 // ---- backward.  A workgroup keeps the gain and the sums of its lanes' columns in registers and takes rows in turn, the next
@@ -485,46 +544,125 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_block_kernel(NormArgs a) {
       }
 }
 
-// Rows longer than that: two walks over the row; the sums of a column are kept in the workgroup's row of the parts.
-template <typename T>
+// Rows longer than that: two walks over R rows side by side; the sums of a column are kept in the workgroup's row of the parts,
+// which is read and written once for the R rows.  Single elements instead of words: 4096 x 16384 fp32 with d_in 1191 us, now 309 (floor
+// 203; eight fp32 words to a lane in registers spill).  One row or four: 1000 x 16384 fp32 104 / 78; up to 512 rows there are
+// too few groups of four for the CUs (600 rows 63 / 44).
+template <typename T, int R>
 __global__ __launch_bounds__(kBlock) void norm_bwd_long_kernel(NormArgs a) {
-  __shared__ float sh[2][kBlock / 64][2];
+  __shared__ float sh[2][kBlock / 64][2 * R];
+  constexpr int kV = 16 / sizeof(T), kU = R == 1 ? 4 : 1;
   const int64_t d = a.d;
   const float inv = 1.f / (float)d;
   float* part = a.parts ? a.parts + (int64_t)blockIdx.x * d : nullptr;
   float* part_b = part ? part + (int64_t)a.part_rows * d : nullptr;
-  if (part && !a.accumulate)
-    for (int64_t c = threadIdx.x; c < d; c += kBlock) part[c] = part_b[c] = 0.f;     // (each element is one thread's own)
+  bool add = a.accumulate;
   int turn = 0;
-  for (int64_t row = blockIdx.x; row < a.rows; row += a.blocks, turn ^= 1) {
-    const T* x = static_cast<const T*>(a.x) + row * a.xs;
-    const T* dy = static_cast<const T*>(a.dy) + row * a.ys;
-    const T* in = a.r ? static_cast<const T*>(a.r) + row * a.rs : nullptr;
-    T* out = static_cast<T*>(a.out) + row * a.os;
-    const float mean = a.mean[row], rstd = a.rstd[row];
-    auto terms = [&](int64_t c, float& n, float& e, float& y) {
-      float g[1] = {1.f};
-      y = (float)dy[c];
-      n = ((float)x[c] - mean) * rstd;
-      if (a.gain) load_gain<T, 1>(a.gain, a.gain_f32, (unsigned)c, g);
-      e = y * g[0];
+  if (part && !add && (int64_t)blockIdx.x * R >= a.rows)         // (no rows at all)
+    for (int64_t c = threadIdx.x; c < d; c += kBlock) part[c] = part_b[c] = 0.f;
+  for (int64_t r0 = (int64_t)blockIdx.x * R; r0 < a.rows; r0 += (int64_t)a.blocks * R, turn ^= 1, add = true) {
+    const int rows = (int)min((int64_t)R, a.rows - r0);
+    float mean[R], rstd[R], s[2 * R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int64_t r = r0 + min(i, rows - 1);
+      mean[i] = a.mean[r];
+      rstd[i] = a.rstd[r];
+      s[2 * i] = s[2 * i + 1] = 0.f;
+    }
+    // row i of a tensor (of those that are not there the last one), found anew: kept, R rows of four tensors spill
+    auto row = [&](auto* base, int64_t stride, int i) {
+      asm volatile("" : "+s"(stride));
+      return base + (r0 + min(i, rows - 1)) * stride;
     };
-    float s[2] = {0.f, 0.f}, n, e, y;
-    for (int64_t c = threadIdx.x; c < d; c += kBlock) {
-      terms(c, n, e, y);
-      s[0] += e;
-      s[1] += e * n;
-    }
-    block_sums<kBlock, 2>(s, sh[turn]);
-    for (int64_t c = threadIdx.x; c < d; c += kBlock) {
-      terms(c, n, e, y);
-      if (part) {
-        part[c] += y * n;
-        part_b[c] += y;
+    const T *xs = static_cast<const T*>(a.x), *dys = static_cast<const T*>(a.dy), *ins = static_cast<const T*>(a.r);
+    auto gain_at = [&](auto v, unsigned at, float* g) {
+      constexpr int V = decltype(v)::value;
+#pragma unroll
+      for (int j = 0; j < V; ++j) g[j] = 1.f;
+      if (a.gain) load_gain<T, V>(a.gain, a.gain_f32, at, g);
+    };
+    walk<kV, kU>(d, [&](auto v, auto& at, auto& there) {
+      constexpr int V = decltype(v)::value, U = std::extent<std::remove_reference_t<decltype(at)>>::value;
+      Pack<T, V> xw[U][R], yw[U][R];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          xw[u][i] = Pack<T, V>::at(row(xs, a.xs, i), at[u]);
+          yw[u][i] = Pack<T, V>::at(row(dys, a.ys, i), at[u]);
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float g[V];
+        gain_at(v, at[u], g);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          float n[V], e[V];
+          xw[u][i].get(n);
+          yw[u][i].get(e);
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            e[j] = there[u] ? e[j] * g[j] : 0.f;
+            s[2 * i] += e[j];
+            s[2 * i + 1] += there[u] ? e[j] * ((n[j] - mean[i]) * rstd[i]) : 0.f;
+          }
+        }
       }
-      const float f = rstd * (e - s[0] * inv - n * (s[1] * inv));
-      out[c] = (T)(in ? (float)in[c] + f : f);
-    }
+    });
+    block_sums<kBlock, 2 * R>(s, sh[turn]);
+#pragma unroll
+    for (int i = 0; i < 2 * R; ++i) s[i] *= inv, here(s[i]);     // (vector registers: the scalar ones are all taken)
+    walk<kV, kU>(d, [&](auto v, auto& at, auto& there) {
+      constexpr int V = decltype(v)::value, U = std::extent<std::remove_reference_t<decltype(at)>>::value;
+      Pack<T, V> xw[U][R], yw[U][R], iw[U][R];
+      Pack<float, V> old[U], old_b[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          xw[u][i] = Pack<T, V>::at(row(xs, a.xs, i), at[u]);
+          yw[u][i] = Pack<T, V>::at(row(dys, a.ys, i), at[u]);
+          if (a.r) iw[u][i] = Pack<T, V>::at(row(ins, a.rs, i), at[u]);
+        }
+        if (part && add) {
+          old[u] = Pack<float, V>::at(part, at[u]);
+          old_b[u] = Pack<float, V>::at(part_b, at[u]);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float g[V], dg[V], db[V];
+        gain_at(v, at[u], g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) dg[j] = db[j] = 0.f;
+        if (part && add) {
+          old[u].get(dg);
+          old_b[u].get(db);
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          float n[V], y[V], f[V];
+          xw[u][i].get(n);
+          yw[u][i].get(y);
+#pragma unroll
+          for (int j = 0; j < V; ++j) f[j] = 0.f;
+          if (a.r) iw[u][i].get(f);
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            n[j] = (n[j] - mean[i]) * rstd[i];
+            dg[j] += i < rows ? y[j] * n[j] : 0.f;
+            db[j] += i < rows ? y[j] : 0.f;
+            f[j] += rstd[i] * (y[j] * g[j] - s[2 * i] - n[j] * s[2 * i + 1]);
+          }
+          if (i < rows && there[u]) Pack<T, V>::of(f).to(row(static_cast<T*>(a.out), a.os, i), at[u]);
+        }
+        if (part && there[u]) {
+          Pack<float, V>::of(dg).to(part, at[u]);
+          Pack<float, V>::of(db).to(part_b, at[u]);
+        }
+      }
+    });
   }
 }
 
@@ -689,8 +827,8 @@ template <typename T, typename F> bool forward_shape(int64_t rows, int64_t d, F 
   if (w <= 2048) return take<V, kBlock, 4>(f);
   return false;
 }
-// Backward: a wavefront up to 256 words, whose sums then take half of its registers; a workgroup beyond.
-template <typename T, typename F> bool backward_shape(int64_t d, F f) {
+// Backward: a wavefront up to 256 words, whose sums then take half of its registers; a workgroup beyond.  FEW: no sums are kept.
+template <typename T, bool FEW = false, typename F> bool backward_shape(int64_t d, F f) {
   constexpr int V = 16 / sizeof(T);
   if (d < V) return take<1, 16, 1>(f);
   const int64_t w = (d + V - 1) / V;
@@ -702,6 +840,8 @@ template <typename T, typename F> bool backward_shape(int64_t d, F f) {
   if (w <= 512) return take<V, kBlock, 1>(f);
   if (w <= 1024) return take<V, kBlock, 2>(f);
   if (w <= 2048) return take<V, kBlock, 4>(f);
+  if constexpr (FEW && sizeof(T) == 4)
+    if (w <= 4096) return take<V, kBlock, 8>(f);
   return false;
 }
 
@@ -734,8 +874,9 @@ template <typename T> int norm_fwd(const NormArgs& a, hipStream_t s) {
 
 template <typename T> constexpr bool ahead(int kb) { return kb < 4 || sizeof(T) == 4; }
 template <typename T> constexpr int rows_at_once(int kb) { return ahead<T>(kb) ? 4 / kb : 2; }
-template <typename T> int rows_of_block(int64_t d) {      // rows that a workgroup of the backward takes at a time
-  int n = 1;
+int rows_of_long(int64_t rows) { return rows <= 2 * SECO_NORM_BLOCKS ? 1 : 4; }   // (see norm_bwd_long_kernel)
+template <typename T> int rows_of_block(int64_t rows, int64_t d) {      // rows that a workgroup of the backward takes at a time
+  int n = rows_of_long(rows);
   backward_shape<T>(d, [&](auto, auto g, auto kb) {
     constexpr int G = decltype(g)::value;
     n = G <= 64 ? kBlock / G : rows_at_once<T>(decltype(kb)::value);
@@ -755,15 +896,15 @@ template <typename T> int norm_bwd(const NormArgs& a, hipStream_t s) {
       else a.r ? launch(norm_bwd_block_kernel<T, V, KB, R, kAhead, true, false>) : launch(norm_bwd_block_kernel<T, V, KB, R, kAhead, false, false>);
     }
   });
-  if (!done) hipLaunchKernelGGL(norm_bwd_long_kernel<T>, dim3(a.blocks), dim3(kBlock), 0, s, a);
+  if (!done) rows_of_long(a.rows) == 1 ? launch(norm_bwd_long_kernel<T, 1>) : launch(norm_bwd_long_kernel<T, 4>);
   return hipGetLastError() == hipSuccess ? SECO_OK : SECO_ERR_LAUNCH;
 }
 
-template <typename T> int norm_bwd_few(NormArgs a, bool rows_too, hipStream_t s) {
-  backward_shape<T>(a.d, [&](auto v, auto g, auto kb) {
+template <typename T> int norm_bwd_few(NormArgs a, bool rows, bool sums, hipStream_t s) {
+  backward_shape<T, true>(a.d, [&](auto v, auto g, auto kb) {
     constexpr int V = decltype(v)::value, G = decltype(g)::value, KB = decltype(kb)::value, kRows = kBlock / G;
-    a.blocks = rows_too ? (int)((a.rows + kRows - 1) / kRows) : 0;
-    const unsigned grid = (unsigned)(a.blocks + (a.d + 4 * V - 1) / (4 * V));
+    a.blocks = rows ? (int)((a.rows + kRows - 1) / kRows) : 0;
+    const unsigned grid = (unsigned)(a.blocks + (sums ? (a.d + 4 * V - 1) / (4 * V) : 0));
     if (a.r) hipLaunchKernelGGL((norm_bwd_few_kernel<T, V, G, KB, true>), dim3(grid), dim3(kBlock), 0, s, a);
     else hipLaunchKernelGGL((norm_bwd_few_kernel<T, V, G, KB, false>), dim3(grid), dim3(kBlock), 0, s, a);
   });
@@ -778,14 +919,14 @@ template <typename T> int norm_bwd_few(NormArgs a, bool rows_too, hipStream_t s)
 // 14.7 / 17.0, 1024 x 8192 (not taken) 27.8 / 28.1, 2048 x 4096 (not taken) 30.5 / 23.5.
 bool norm_few(int64_t rows, int64_t d, int dtype) {
   const int64_t elem = dtype == SECO_BF16 ? 2 : 4;
-  return rows >= 1 && rows <= 1024 && d * elem <= 32768 && rows * d * elem <= (int64_t)16 << 20;   // (32768: backward_shape's longest)
+  return rows >= 1 && rows <= 1024 && d <= 16384 && rows * d * elem <= (int64_t)16 << 20;   // (16384: backward_shape's longest)
 }
-int launch_norm_bwd_few(const NormArgs& a, bool rows_too, hipStream_t s) {
-  return a.dtype == SECO_BF16 ? norm_bwd_few<__bf16>(a, rows_too, s) : norm_bwd_few<float>(a, rows_too, s);
+int launch_norm_bwd_few(const NormArgs& a, bool rows, bool sums, hipStream_t s) {
+  return a.dtype == SECO_BF16 ? norm_bwd_few<__bf16>(a, rows, sums, s) : norm_bwd_few<float>(a, rows, sums, s);
 }
 
 int norm_blocks(int64_t rows, int64_t d, int dtype) {
-  const int per = dtype == SECO_BF16 ? rows_of_block<__bf16>(d) : rows_of_block<float>(d);
+  const int per = dtype == SECO_BF16 ? rows_of_block<__bf16>(rows, d) : rows_of_block<float>(rows, d);
   const int64_t n = (rows + per - 1) / per;
   return (int)(n < 1 ? 1 : n < SECO_NORM_BLOCKS ? n : SECO_NORM_BLOCKS);
 }

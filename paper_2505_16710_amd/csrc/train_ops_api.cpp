@@ -256,8 +256,8 @@ extern "C" int layer_norm_bwd(const layer_norm_desc* desc, const void* x, const 
     a.d_gain = d_gain;
     a.d_bias = d_bias;
     const bool apart = !overlap(desc, d_x, x, desc->x_stride) && !overlap(desc, d_x, d_y, desc->y_stride);
-    rc = launch_norm_bwd_few(a, apart, s);
-    return rc || apart ? rc : launch_norm_bwd(a, s);
+    rc = launch_norm_bwd_few(a, apart, true, s);
+    return rc || apart ? rc : launch_norm_bwd_few(a, true, false, s);
   }
   a.parts = sums ? static_cast<float*>(ws) : nullptr;
   rc = launch_norm_bwd(a, s);
@@ -375,7 +375,7 @@ extern "C" int dec_layer_norm_bwd(int dtype, const void* x, const void* gain, co
   if (norm_few(rows, d, dtype)) {                // (into the first share; d_x overwrites neither x nor d_h here)
     a.d_gain = parts;
     a.d_bias = parts + SECO_NORM_BLOCKS * d;
-    return launch_norm_bwd_few(a, true, static_cast<hipStream_t>(stream));
+    return launch_norm_bwd_few(a, true, true, static_cast<hipStream_t>(stream));
   }
   a.parts = parts;
   a.blocks = norm_blocks(rows, d, dtype);

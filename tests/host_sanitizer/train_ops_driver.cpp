@@ -22,7 +22,7 @@
 namespace {
 struct Log {
   std::vector<seco::NormArgs> fwd, bwd, few;
-  std::vector<bool> rows_too;
+  std::vector<std::pair<bool, bool>> parts_of;
   int sums = 0, counts = 0;
   std::vector<std::pair<int, seco::AdamArgs>> adam;
   std::vector<seco::RopeAxesArgs> rope;
@@ -35,9 +35,9 @@ int norm_blocks(int64_t rows, int64_t, int) { return rows < 1 ? 1 : rows < SECO_
 bool norm_few(int64_t rows, int64_t d, int) { return rows >= 1 && rows <= 1024 && d <= 16384; }
 int launch_norm_fwd(const NormArgs& a, hipStream_t) { log_.fwd.push_back(a); return SECO_OK; }
 int launch_norm_bwd(const NormArgs& a, hipStream_t) { log_.bwd.push_back(a); return SECO_OK; }
-int launch_norm_bwd_few(const NormArgs& a, bool rows_too, hipStream_t) {
+int launch_norm_bwd_few(const NormArgs& a, bool rows, bool sums, hipStream_t) {
   log_.few.push_back(a);
-  log_.rows_too.push_back(rows_too);
+  log_.parts_of.emplace_back(rows, sums);
   return SECO_OK;
 }
 int launch_norm_sums(const float*, int, int64_t, void*, void*, int, hipStream_t) { log_.sums++; return SECO_OK; }
@@ -62,8 +62,8 @@ static void layer_norms() {
   for (auto [dx, apart] : {std::pair<uintptr_t, bool>{0x300000, true}, {0x100000, false}, {0x200000, false}, {0x100000 + span - 2, false},
                            {0x100000 + span, true}, {0x100000 - span, true}, {0x100000 - span + 2, false}}) {
     log_ = Log{};
-    CHECK(bwd(dx) == SECO_OK && log_.few.size() == 1 && log_.rows_too[0] == apart && log_.bwd.size() == (apart ? 0u : 1u) && log_.sums == 0);
-    CHECK(apart || log_.bwd[0].parts == nullptr);
+    CHECK(bwd(dx) == SECO_OK && log_.few.size() == (apart ? 1u : 2u) && log_.bwd.empty() && log_.sums == 0);
+    CHECK(log_.parts_of[0].first == apart && log_.parts_of[0].second && (apart || (log_.parts_of[1].first && !log_.parts_of[1].second)));
   }
   d.rows = 5000;
   log_ = Log{};

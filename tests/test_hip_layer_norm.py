@@ -93,6 +93,10 @@ def test_forward(t, d, residual):
 def test_backward(t, d, rows, d_in):
     if rows * d > 1 << 21:
         rows = max(2, (1 << 21) // d)
+    _check_backward(t, d, rows, d_in)
+
+
+def _check_backward(t, d, rows, d_in):
     dtype = TYPES[t]
     x, dy, extra = _rows(d + 4, rows, d, dtype, 2), _rows(d + 5, rows, d, dtype), _rows(d + 6, rows, d, dtype)
     gain = _rows(d + 7, 1, d, dtype)[0].contiguous() + 1
@@ -117,8 +121,15 @@ def test_backward(t, d, rows, d_in):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t,d,rows,d_in", [("f32", 8197, 1027, "in place"), ("f32", 16384, 100, "apart"), ("f32", 12003, 300, "none"),
+                                           ("bf16", 16400, 1030, "none"), ("bf16", 16411, 1301, "apart"), ("f32", 16385, 768, "in place")])
+def test_backward_of_long_rows(t, d, rows, d_in):
+    _check_backward(t, d, rows, d_in)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("t", ["bf16", "f32"])
-@pytest.mark.parametrize("rows,d", [(1, 3), (2, 1024), (129, 45), (513, 260), (1024, 1027), (1025, 1027), (300, 16384), (40, 16390)])
+@pytest.mark.parametrize("rows,d", [(1, 3), (2, 1024), (129, 45), (513, 260), (1024, 1027), (1025, 1027), (300, 16384), (40, 16390), (100, 12001), (1040, 16391)])
 def test_where_the_results_lie_changes_nothing(t, rows, d):
     """d_x apart, in the place of x, of d_y or (one row apart in the same buffer) beside x: the same bits; one sum without the other."""
     dtype = TYPES[t]
