@@ -35,7 +35,7 @@ int launch_norm_fwd(const NormArgs& a, hipStream_t s);
 int launch_norm_bwd(const NormArgs& a, hipStream_t s);
 // Whether a backward call has so few rows that its sums need no parts, but come from a.x and a.dy a second time; and that call:
 // d_x (rows), the sums, or both in one launch where d_x overwrites neither
-bool norm_few(int64_t rows, int64_t d, int dtype);
+bool norm_few(int64_t rows, int64_t d);
 int launch_norm_bwd_few(const NormArgs& a, bool rows, bool sums, hipStream_t s);
 // d_gain, d_bias (either NULL) = parts added up over the blocks in their order
 int launch_norm_sums(const float* parts, int blocks, int64_t d, void* d_gain, void* d_bias, int gain_f32, hipStream_t s);

@@ -200,7 +200,7 @@ extern "C" int rope_readout_axes(const seco_desc* desc, const rope_axes* axes, c
 
 extern "C" size_t layer_norm_workspace_bytes(const layer_norm_desc* desc) {
   if (check_norm(desc)) return (size_t)-1;
-  if (norm_few(desc->rows, desc->d, desc->dtype)) return 0;
+  if (norm_few(desc->rows, desc->d)) return 0;
   return (size_t)2 * norm_blocks(desc->rows, desc->d, desc->dtype) * desc->d * sizeof(float);
 }
 
@@ -239,7 +239,7 @@ extern "C" int layer_norm_bwd(const layer_norm_desc* desc, const void* x, const 
   if (!aligned(gain, ge) || !aligned(d_gain, ge) || !aligned(d_bias, ge) || !aligned(mean, 4) || !aligned(rstd, 4)) return SECO_ERR_ALIGN;
   if (!rows_apart(desc, desc->out_stride)) return SECO_ERR_SHAPE;
   const bool sums = d_gain || d_bias;
-  const bool few = sums && norm_few(desc->rows, desc->d, desc->dtype);
+  const bool few = sums && norm_few(desc->rows, desc->d);
   if (sums && !few && (!ws || !aligned(ws, 16) || ws_bytes < layer_norm_workspace_bytes(desc))) return SECO_ERR_WORKSPACE;
   if (desc->rows == 0 && !sums) return SECO_OK;
   NormArgs a = norm_args(desc);
@@ -372,7 +372,7 @@ extern "C" int dec_layer_norm_bwd(int dtype, const void* x, const void* gain, co
   a.rstd = const_cast<float*>(rstd);
   a.part_rows = SECO_NORM_BLOCKS;
   a.accumulate = 1;
-  if (norm_few(rows, d, dtype)) {                // (into the first share; d_x overwrites neither x nor d_h here)
+  if (norm_few(rows, d)) {                // (into the first share; d_x overwrites neither x nor d_h here)
     a.d_gain = parts;
     a.d_bias = parts + SECO_NORM_BLOCKS * d;
     return launch_norm_bwd_few(a, true, true, static_cast<hipStream_t>(stream));

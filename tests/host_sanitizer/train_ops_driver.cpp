@@ -32,7 +32,7 @@ template <typename T = void> T* at(uintptr_t p) { return reinterpret_cast<T*>(p)
 
 namespace seco {
 int norm_blocks(int64_t rows, int64_t, int) { return rows < 1 ? 1 : rows < SECO_NORM_BLOCKS ? (int)rows : SECO_NORM_BLOCKS; }
-bool norm_few(int64_t rows, int64_t d, int) { return rows >= 1 && rows <= 1024 && d <= 16384; }
+bool norm_few(int64_t rows, int64_t d) { return rows >= 1 && rows <= 1024 && d <= 16384; }
 int launch_norm_fwd(const NormArgs& a, hipStream_t) { log_.fwd.push_back(a); return SECO_OK; }
 int launch_norm_bwd(const NormArgs& a, hipStream_t) { log_.bwd.push_back(a); return SECO_OK; }
 int launch_norm_bwd_few(const NormArgs& a, bool rows, bool sums, hipStream_t) {

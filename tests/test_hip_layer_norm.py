@@ -89,10 +89,10 @@ def test_forward(t, d, residual):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("t,d", CASES)
-@pytest.mark.parametrize("rows,d_in", [(1, "none"), (7, "in place"), (300, "apart"), (1030, "none")])
+@pytest.mark.parametrize("rows,d_in", [(1, "none"), (7, "in place"), (300, "apart"), (1030, "none"), (1301, "apart")])
 def test_backward(t, d, rows, d_in):
-    if rows * d > 1 << 21:
-        rows = max(2, (1 << 21) // d)
+    if rows * d > 1 << 22:
+        rows = max(2, (1 << 22) // d)
     _check_backward(t, d, rows, d_in)
 
 
@@ -129,7 +129,7 @@ def test_backward_of_long_rows(t, d, rows, d_in):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("t", ["bf16", "f32"])
-@pytest.mark.parametrize("rows,d", [(1, 3), (2, 1024), (129, 45), (513, 260), (1024, 1027), (1025, 1027), (300, 16384), (40, 16390), (100, 12001), (1040, 16391)])
+@pytest.mark.parametrize("rows,d", [(1, 3), (2, 1024), (129, 45), (513, 260), (1024, 1027), (1280, 1027), (1281, 1027), (1900, 333), (1400, 4100), (300, 16384), (40, 16390), (100, 12001), (1040, 16391)])
 def test_where_the_results_lie_changes_nothing(t, rows, d):
     """d_x apart, in the place of x, of d_y or (one row apart in the same buffer) beside x: the same bits; one sum without the other."""
     dtype = TYPES[t]
@@ -166,10 +166,11 @@ def test_gradient_added_in_place(t, rows, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows", [700, 1500])
 @pytest.mark.parametrize("t,d", [("bf16", 1024), ("bf16", 4096), ("bf16", 130), ("bf16", 20001), ("f32", 8192), ("f32", 63)])
-def test_results_are_the_same_every_time(t, d):
+def test_results_are_the_same_every_time(t, d, rows):
     dtype = TYPES[t]
-    x, dy = _on_gpu(_rows(1, 700, d, dtype)), _on_gpu(_rows(2, 700, d, dtype))
+    x, dy = _on_gpu(_rows(1, rows, d, dtype)), _on_gpu(_rows(2, rows, d, dtype))
     gain = torch.ones(d, dtype=dtype, device=DEV)
     y, mean, rstd = seco.layer_norm_fwd(x, gain)
     first = seco.layer_norm_bwd(x, gain, mean, rstd, dy)
@@ -289,7 +290,7 @@ def test_layouts(d):
 @pytest.mark.gpu
 @pytest.mark.parametrize("t,d", [("bf16", 5), ("bf16", 100), ("bf16", 250), ("bf16", 1027), ("bf16", 2048), ("bf16", 4100), ("bf16", 8200),
                                  ("bf16", 20001), ("f32", 1027), ("f32", 4096), ("f32", 8000)])
-@pytest.mark.parametrize("rows", [1, 2, 5, 31, 1030])
+@pytest.mark.parametrize("rows", [1, 2, 5, 31, 1030, 1300])
 def test_what_lies_behind_the_rows_stays(t, d, rows):
     dtype = TYPES[t]
     rows = min(rows, max(2, (1 << 21) // d))
@@ -461,8 +462,8 @@ def test_status_codes():
     assert bwd(many, ws=None) == -6 and bwd(many, n=16) == -6 and bwd(many, ws=C.c_void_p(0x1008)) == -6
     assert bwd(desc(), dx=None) == -1 and bwd(desc(), dg=C.c_void_p(0x1001)) == -5
     lib.layer_norm_workspace_bytes.restype = C.c_size_t
-    assert lib.layer_norm_workspace_bytes(C.byref(desc())) == 0 and lib.layer_norm_workspace_bytes(C.byref(desc(rows=1024))) == 0
+    assert lib.layer_norm_workspace_bytes(C.byref(desc())) == 0 and lib.layer_norm_workspace_bytes(C.byref(desc(rows=1280))) == 0
     assert lib.layer_norm_workspace_bytes(C.byref(desc(rows=0))) == 2 * 16 * 4
-    assert lib.layer_norm_workspace_bytes(C.byref(desc(rows=1025))) > 0 and lib.layer_norm_workspace_bytes(C.byref(desc(d=16385))) > 0
+    assert lib.layer_norm_workspace_bytes(C.byref(desc(rows=1281))) > 0 and lib.layer_norm_workspace_bytes(C.byref(desc(d=16385))) > 0
     assert lib.layer_norm_workspace_bytes(C.byref(desc(rows=100000))) == 2 * 256 * 16 * 4
     assert lib.layer_norm_workspace_bytes(C.byref(desc(d=-1))) == C.c_size_t(-1).value
