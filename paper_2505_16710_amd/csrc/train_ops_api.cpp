@@ -273,8 +273,11 @@ extern "C" int adamw_step(const adamw_desc* desc, const adamw_tensor* tensors_ho
       desc->eps < 0.0)
     return SECO_ERR_RANGE;
   if (!aligned(step, 8) || !aligned(desc->lr_device, 4) || !aligned(desc->grad_scale_device, 4)) return SECO_ERR_ALIGN;
-  for (int32_t i = 0; i < n_tensors; ++i)
+  unsigned kinds = 0;                            // that there are
+  for (int32_t i = 0; i < n_tensors; ++i) {
     if (const int rc = check_adamw(desc, tensors_host[i])) return rc;
+    kinds |= 1u << kind_of(desc, tensors_host[i]);
+  }
   AdamArgs a{};
   a.lr = desc->lr;
   a.beta1 = desc->beta1;
@@ -294,7 +297,7 @@ extern "C" int adamw_step(const adamw_desc* desc, const adamw_tensor* tensors_ho
   // Tensors of one kind share launches; one that is full waits for the next tensor, so that the last launch is known as such.
   int pending = 0, rc = SECO_OK;
   for (int kind = 0; kind < 16 && !rc; ++kind)
-    for (int32_t i = 0; i < n_tensors && !rc; ++i) {
+    for (int32_t i = 0; kinds >> kind & 1 && i < n_tensors && !rc; ++i) {
       const adamw_tensor& t = tensors_host[i];
       if (t.n == 0 || kind_of(desc, t) != kind) continue;
       const uint32_t spans = (uint32_t)((t.n + span - 1) / span);      // at most 2^30

@@ -216,6 +216,24 @@ const float* scalar_on(const Tensor& t, const Tensor& like_t, const char* what) 
   return fptr(t);
 }
 
+// Sorts by merging the runs that are in order already: tensors that were made one behind the other mostly are.
+void in_order(std::vector<std::pair<uintptr_t, uintptr_t>>& a) {
+  std::vector<size_t> ends;                      // of the runs
+  for (size_t i = 1; i <= a.size(); ++i)
+    if (i == a.size() || a[i] < a[i - 1]) ends.push_back(i);
+  std::vector<std::pair<uintptr_t, uintptr_t>> b(a.size());
+  while (ends.size() > 1) {
+    size_t begin = 0, kept = 0;
+    for (size_t i = 0; i < ends.size(); i += 2) {
+      const size_t end = ends[std::min(i + 1, ends.size() - 1)];
+      std::merge(a.begin() + begin, a.begin() + ends[i], a.begin() + ends[i], a.begin() + end, b.begin() + begin);
+      ends[kept++] = begin = end;
+    }
+    ends.resize(kept);
+    a.swap(b);
+  }
+}
+
 // (params, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, masters, m_scales, v_scales, grad_scale, stream)
 PyObject* adamw(PyObject* const* a) {
   const Sequence params(a[0]), grads(a[1]), ms(a[2]), vs(a[3]), masters(a[10]),
@@ -241,11 +259,6 @@ PyObject* adamw(PyObject* const* a) {
   d.eps = real(a[8]);
   d.state_bits = eight ? 8 : 32;
   const auto list = std::make_unique<adamw_tensor[]>((size_t)n);
-  std::vector<std::pair<uintptr_t, uintptr_t>> places;
-  places.reserve((size_t)n * 6);
-  auto written = [&](const Tensor& x) {
-    if (x.numel() > 0) places.emplace_back((uintptr_t)ptr(x), (uintptr_t)ptr(x) + nbytes(x));
-  };
   for (Py_ssize_t i = 0; i < n; ++i) {
     const Tensor &p = params[i], &g = grads[i], &m = ms[i], &v = vs[i];
     adamw_tensor& t = list[i];
@@ -274,21 +287,30 @@ PyObject* adamw(PyObject* const* a) {
           bad(PyExc_ValueError, "m_scales, v_scales", i, "one contiguous float32 per 256 elements of the parameter");
       t.m_scale = fptr(m_scales[i]);
       t.v_scale = fptr(v_scales[i]);
-      written(m_scales[i]);
-      written(v_scales[i]);
     }
     if (masters.s && masters.item(i) != Py_None) {
       const Tensor& w = masters[i];
       if (w.scalar_type() != at::kFloat || p.scalar_type() != at::kBFloat16) bad(PyExc_TypeError, "masters", i, "float32, of bfloat16 parameters only");
       same_places(w, p, "masters", i);
       t.master = fptr(w);
-      written(w);
     }
-    written(p);
-    written(m);
-    written(v);
   }
-  std::sort(places.begin(), places.end());
+  std::vector<std::pair<uintptr_t, uintptr_t>> places;        // of what is written
+  places.reserve((size_t)n * 6);
+  auto written = [&](auto where) {
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      const std::pair<void*, int64_t> w = where(list[i]);
+      if (w.first && w.second > 0) places.emplace_back((uintptr_t)w.first, (uintptr_t)w.first + (uintptr_t)w.second);
+    }
+  };
+  typedef std::pair<void*, int64_t> Place;
+  written([](const adamw_tensor& t) { return Place(t.param, t.n * (t.param_dtype == SECO_BF16 ? 2 : 4)); });
+  written([&](const adamw_tensor& t) { return Place(t.m, t.n * (eight ? 1 : 4)); });
+  written([&](const adamw_tensor& t) { return Place(t.v, t.n * (eight ? 1 : 4)); });
+  written([](const adamw_tensor& t) { return Place(t.m_scale, (t.n + 255) / 256 * 4); });
+  written([](const adamw_tensor& t) { return Place(t.v_scale, (t.n + 255) / 256 * 4); });
+  written([](const adamw_tensor& t) { return Place(t.master, t.n * 4); });
+  in_order(places);
   for (size_t i = 1; i < places.size(); ++i)
     if (places[i].first < places[i - 1].second) raise(PyExc_ValueError, "params and their states: two of them overlap, or one is there twice");
   if (!step.is_cuda()) raise(PyExc_ValueError, "the tensors must be on one GPU");
