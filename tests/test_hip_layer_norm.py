@@ -350,9 +350,10 @@ def test_more_rows_than_a_grid_holds_along_x():
 
 
 @pytest.mark.gpu
-def test_captured_and_replayed():
-    x, dy = _rows(70, 300, 1024, torch.bfloat16).to(DEV), _rows(71, 300, 1024, torch.bfloat16).to(DEV)
-    gain = torch.ones(1024, dtype=torch.bfloat16, device=DEV)
+@pytest.mark.parametrize("rows,d", [(300, 1024), (1500, 1024), (1400, 4099), (30, 20001)])
+def test_captured_and_replayed(rows, d):
+    x, dy = _rows(70, rows, d, torch.bfloat16).to(DEV), _rows(71, rows, d, torch.bfloat16).to(DEV)
+    gain = torch.ones(d, dtype=torch.bfloat16, device=DEV)
 
     def both():
         y, mean, rstd = seco.layer_norm_fwd(x, gain)
@@ -367,6 +368,35 @@ def test_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, both()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [300, 1500])
+def test_two_graphs_side_by_side(rows):
+    """Two captured backwards replayed at once on two streams: each has its own shares and sums."""
+    gain = torch.ones(1024, dtype=torch.bfloat16, device=DEV)
+    graphs, outs, want, streams = [], [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for i in range(2):
+        x, dy = _rows(72 + i, rows, 1024, torch.bfloat16).to(DEV), _rows(74 + i, rows, 1024, torch.bfloat16).to(DEV)
+        _, mean, rstd = seco.layer_norm_fwd(x, gain)
+        want.append(seco.layer_norm_bwd(x, gain, mean, rstd, dy))
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for _ in range(10):
+                out = seco.layer_norm_bwd(x, gain, mean, rstd, dy)
+        graphs.append((graph, x, dy, mean, rstd))
+        outs.append(out)
+    for _ in range(3):
+        for t in outs[0] + outs[1]:
+            t.zero_()
+        torch.cuda.synchronize()
+        for (graph, *_), stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for out, ref in zip(outs, want):
+            assert all(torch.equal(a, b) for a, b in zip(out, ref))
 
 
 @pytest.mark.gpu

@@ -104,6 +104,15 @@ def test_layer_norms_without_biases_and_one_gain_for_all_columns():
 
 
 @pytest.mark.gpu
+def test_long_and_short_chunks():
+    """2600 rows to a chunk, then 800: the norms' gradients are formed in two ways, and added up."""
+    cfg, p64, params, dec, tok, tgt, pos = _setup(25, 2, 1700, torch.float32, **_options("both", torch.float32))
+    _, ref = om.monolithic_grads(cfg, p64, tok, tgt, pos)
+    _, got = dec.step(tok.to(DEV), tgt.to(DEV), 1300, positions=pos.to(DEV))
+    _compare(ref, got, 5e-4)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("layers", [0, 1])
 def test_few_layers(layers, monkeypatch):
     for sizes in (F32, BF16):
