@@ -174,27 +174,28 @@ class LayerNorm(torch.autograd.Function):
 
 
 def hand_over(params, grads):
-    """Leaves every parameter's gradient in .grad (None there if no chunk reached it) and returns {name: gradient}, zeros
-    for those.  A tensor under several names gets the sum over them.  A parameter that something waits for (hooks of
-    the tensor, post-accumulate hooks, hooks of its accumulation node) receives its gradient through autograd, which
-    runs them: once per step, with the step's gradient.
-    So does a parameter that is computed from others."""
+    """Leaves every parameter's gradient in .grad, in the place of what was there (None there if no chunk reached it), and
+    returns {name: gradient}, zeros for those.  A tensor under several names gets the sum over them.  A parameter that
+    something waits for (hooks of the tensor, post-accumulate hooks, hooks of its accumulation node) receives its gradient
+    through autograd, which runs them: once per step, with the step's gradient.
+    So does a parameter that is computed from others; the leaves behind it take what reaches them as they do in backward(),
+    on top of what they hold and, if they are parameters too, of their own gradient."""
     has_grad_hooks = (_b._ext or _b._load_ext()).has_grad_hooks
     total = {}                                  # id -> gradient
     for n, t in params.items():
         g = grads.get(n)
         if g is not None and t.requires_grad:
             total[id(t)] = total[id(t)] + g if id(t) in total else g
-    done = set()
+    roots = {}                                  # id -> parameter: what takes its gradient through autograd
     for t in params.values():
-        g = total.get(id(t))
-        if g is None or id(t) in done:
-            continue
-        done.add(id(t))
-        if t.is_leaf and not has_grad_hooks(t):
-            t.grad = g
-        else:
-            torch.autograd.backward(t, g)
+        if id(t) in total:
+            plain = t.is_leaf and not has_grad_hooks(t)
+            if t.is_leaf:
+                t.grad = total[id(t)] if plain else None
+            if not plain:
+                roots[id(t)] = t
+    if roots:                                   # (in one pass, behind all assignments: no order of the names loses a share)
+        torch.autograd.backward(list(roots.values()), [total[i] for i in roots])
     out = {}
     for n, t in params.items():
         g = total.get(id(t))

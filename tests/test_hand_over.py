@@ -1,4 +1,5 @@
 """How the training step leaves gradients at the parameters (chunk_loop.hand_over); no GPU needed."""
+import pytest
 import torch
 
 from paper_2505_16710_amd.chunk_loop import hand_over
@@ -45,3 +46,39 @@ def test_a_computed_parameter_passes_its_gradient_on():
     a = _leaf(1.0)
     out = hand_over({"w": 2 * a}, {"w": torch.ones(3)})
     assert torch.equal(a.grad, torch.full((3,), 2.0)) and torch.equal(out["w"], torch.ones(3))
+
+
+def test_a_second_step_takes_the_place_of_the_first():
+    a, b, c = _leaf(), _leaf(), _leaf()
+    a.register_hook(lambda g: 10 * g)
+    b.register_post_accumulate_grad_hook(lambda t: None)
+    for k in (1.0, 2.0):
+        out = hand_over({"a": a, "b": b, "c": c}, {n: torch.full((3,), k) for n in "abc"})
+        assert torch.equal(a.grad, torch.full((3,), 10 * k)) and torch.equal(out["a"], a.grad)
+        assert torch.equal(b.grad, torch.full((3,), k)) and torch.equal(c.grad, torch.full((3,), k))
+
+
+@pytest.mark.parametrize("hooked", [False, True])
+@pytest.mark.parametrize("order", [("emb", "head"), ("head", "emb")])
+def test_a_parameter_beside_one_computed_from_it(order, hooked):
+    """Tied weights: the leaf holds both shares, whichever name comes first; its hook runs once, with the sum."""
+    emb, seen = torch.zeros(2, 3, requires_grad=True), []
+    if hooked:
+        emb.register_hook(lambda g: seen.append(g.clone()))
+    for _ in range(2):
+        p, g = {"emb": emb, "head": emb.t()}, {"emb": torch.ones(2, 3), "head": torch.full((3, 2), 2.0)}
+        out = hand_over({n: p[n] for n in order}, g)
+        assert torch.equal(emb.grad, torch.full((2, 3), 3.0)) and torch.equal(out["emb"], emb.grad)
+        assert torch.equal(out["head"], g["head"])
+    assert len(seen) == 2 * hooked and all(torch.equal(x, torch.full((2, 3), 3.0)) for x in seen)
+
+
+def test_parameters_computed_by_one_operation():
+    """Two pieces of a product: one backward pass, which would find the product's factors gone the second time."""
+    a = _leaf(2.0)
+    x, y = torch.stack([a * a, 3 * a]).unbind()
+    hand_over({"x": x, "y": y}, {"x": torch.ones(3), "y": torch.ones(3)})
+    assert torch.equal(a.grad, torch.full((3,), 7.0))
+    u = (a * a).view(3, 1)
+    hand_over({"first": u[:1], "rest": u[1:]}, {"first": torch.ones(1, 1), "rest": torch.ones(2, 1)})
+    assert torch.equal(a.grad, torch.full((3,), 11.0))              # (a is no parameter: what it holds is the program's to clear)
