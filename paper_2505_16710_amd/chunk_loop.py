@@ -205,6 +205,20 @@ def hand_over(params, grads):
     return out
 
 
+def leaves_behind(params):
+    """The leaves that the computed ones among these tensors pass their gradients to."""
+    todo, seen, found = [t.grad_fn for t in params], set(), []
+    while todo:
+        node = todo.pop()
+        if node is None or node in seen:
+            continue
+        seen.add(node)
+        if hasattr(node, "variable"):
+            found.append(node.variable)
+        todo.extend(fn for fn, _ in node.next_functions)
+    return found
+
+
 class ChunkedDecoder:
     """Holds the parameters (dict name -> leaf tensor on the GPU) and runs SeCO / SpaCO steps.
 
@@ -253,8 +267,8 @@ class ChunkedDecoder:
         spaco_chunk_attn_bwd_gather; bf16 parameters): same gradients up to the order of summation.
         positions: with rope_axes, int64 [axes, batch or 1, tokens], every token's position on each axis (default: its number in
         the sequence on all of them).
-        optimizer: an optimizer.AdamW over these parameters, whose step is taken with the step's gradients (not if a token lies
-        outside the table)."""
+        optimizer: an optimizer.AdamW over these parameters (of a computed one: over the leaves behind it), whose step is taken
+        with the step's gradients, what .grad held before left out (not taken if a token lies outside the table)."""
         p = self.p
         B, N = tokens.shape
         dtype, dev = p["emb"].dtype, p["emb"].device
@@ -286,6 +300,11 @@ class ChunkedDecoder:
                 raise ValueError("Alg. 2 in the transposed order needs a chunk length that is a multiple of 64")
         for t in p.values():
             t.grad = None
+        if optimizer is not None:               # (of computed parameters it holds the leaves, which would add up over the steps)
+            its = {id(t) for t in optimizer.params}
+            for t in leaves_behind(p.values()):
+                if id(t) in its:
+                    t.grad = None
         c1 = stage1_chunk_len or chunk_len
         picked = None if selected is None else {int(i) for i in selected}
         order = range(len(starts) - 1, -1, -1) if selected is None else sorted(picked, reverse=True)

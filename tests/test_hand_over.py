@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_2505_16710_amd.chunk_loop import hand_over
+from paper_2505_16710_amd.chunk_loop import hand_over, leaves_behind
 
 
 def _leaf(v=0.0):
@@ -82,3 +82,11 @@ def test_parameters_computed_by_one_operation():
     u = (a * a).view(3, 1)
     hand_over({"first": u[:1], "rest": u[1:]}, {"first": torch.ones(1, 1), "rest": torch.ones(2, 1)})
     assert torch.equal(a.grad, torch.full((3,), 11.0))              # (a is no parameter: what it holds is the program's to clear)
+
+
+def test_leaves_behind_computed_parameters():
+    a, b, c, d = _leaf(), _leaf(), _leaf(), _leaf()
+    s = a * b
+    found = leaves_behind([s[:2], s + c.detach(), d, torch.zeros(3), a.detach()])
+    assert len(found) == 2 and {id(t) for t in found} == {id(a), id(b)}
+    assert leaves_behind([d, c]) == []

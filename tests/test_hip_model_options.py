@@ -202,6 +202,41 @@ def test_a_token_outside_the_table_updates_nothing():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_updates_of_parameters_with_hooks(bits):
+    """Gradients that come through autograd are the step's own, step after step: the same bits as without hooks."""
+    from paper_2505_16710_amd.optimizer import AdamW
+    ends = []
+    for hooked in (False, True):
+        cfg, p64, params, dec, tok, tgt, pos = _setup(17, 1, 96, torch.float32, **_options("both", torch.float32))
+        if hooked:
+            params["l0.wq"].register_hook(lambda g: None)
+            params["l1.norm1_b"].register_post_accumulate_grad_hook(lambda t: None)
+        opt = AdamW(params, lr=1e-2, state_bits=bits)
+        for _ in range(3):
+            dec.step(tok.to(DEV), tgt.to(DEV), 32, positions=pos.to(DEV), optimizer=opt)
+        ends.append({n: t.detach().clone() for n, t in params.items()})
+    assert all(torch.equal(ends[0][n], ends[1][n]) for n in ends[0])
+
+
+@pytest.mark.gpu
+def test_updates_of_leaves_behind_computed_parameters():
+    """A matrix computed from a leaf, anew for every step: the optimizer's leaf holds the last step's gradient alone; one that
+    the optimizer does not hold adds up, as in backward()."""
+    from paper_2505_16710_amd.optimizer import AdamW
+    cfg, p64, params, dec, tok, tgt, pos = _setup(19, 1, 96, torch.float32, **_options("layer", torch.float32))
+    base, other = (params[n].detach().clone().requires_grad_() for n in ("l0.w1", "l0.w2"))
+    opt = AdamW({**{n: t for n, t in params.items() if n not in ("l0.w1", "l0.w2")}, "base": base}, lr=1e-2)
+    total = torch.zeros_like(other)
+    for _ in range(3):
+        params["l0.w1"], params["l0.w2"] = 2 * base, 1 * other
+        _, grads = dec.step(tok.to(DEV), tgt.to(DEV), 32, optimizer=opt)
+        assert torch.equal(base.grad, 2 * grads["l0.w1"])
+        total += grads["l0.w2"]
+        assert torch.equal(other.grad, total)
+
+
+@pytest.mark.gpu
 def test_functions_for_autograd():
     """LayerNorm and RopeMulti inside a graph of framework operators: gradients against the same formulas in 64 bits."""
     from paper_2505_16710_amd.chunk_loop import LayerNorm, RopeMulti
