@@ -89,6 +89,11 @@ template <bool FAR, typename T, int V> __device__ __forceinline__ void word_to(c
   else w.to(row, c);
 }
 
+// Statistics of a row.  One that holds a NaN or an infinity has an rstd of NaN, as the formula gives it (a maximum with zero would
+// take the zero), and a mean of its sum, whose deviations are NaN.
+__device__ __forceinline__ float rstd_of(float var, float eps) { return 1.f / sqrtf((var < 0.f ? 0.f : var) + eps); }
+__device__ __forceinline__ float mean_of(float m0, float delta) { return fabsf(m0) < INFINITY ? m0 + delta : m0; }
+
 // ---- forward: G lanes to a row, KB words of V elements to a lane
 template <typename T, int V, int G, int KB, bool FAR>
 __global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_kernel(NormArgs a) {
@@ -156,9 +161,9 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_kernel(NormArgs a)
   } else {
     block_sums<G, 2>(two, sh[1]);
   }
-  const float delta = two[0] * inv, var = fmaxf(two[1] * inv - delta * delta, 0.f), rstd = 1.f / sqrtf(var + a.eps);
+  const float delta = two[0] * inv, rstd = rstd_of(two[1] * inv - delta * delta, a.eps);
   if (lane == 0) {
-    a.mean[row] = m0 + delta;
+    a.mean[row] = mean_of(m0, delta);
     a.rstd[row] = rstd;
   }
   T* y = static_cast<T*>(a.y) + row * a.ys;
@@ -268,9 +273,9 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_long_kernel(NormArgs a) {
     }
   });
   block_sums<kBlock, 2>(two, sh[1]);
-  const float delta = two[0] * inv, var = fmaxf(two[1] * inv - delta * delta, 0.f), rstd = 1.f / sqrtf(var + a.eps);
+  const float delta = two[0] * inv, rstd = rstd_of(two[1] * inv - delta * delta, a.eps);
   if (threadIdx.x == 0) {
-    a.mean[row] = m0 + delta;
+    a.mean[row] = mean_of(m0, delta);
     a.rstd[row] = rstd;
   }
   T* y = static_cast<T*>(a.y) + row * a.ys;

@@ -246,6 +246,25 @@ def test_infinities_and_nan_stay_in_their_row(t, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t,d", [("bf16", 5), ("bf16", 96), ("bf16", 1024), ("bf16", 1027), ("bf16", 5000), ("f32", 4096), ("f32", 17000)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_statistics_of_rows_that_are_not_finite(t, d, residual):
+    """The formulas': rstd is NaN, the mean the infinity of the row's sum, or NaN."""
+    dtype, inf = TYPES[t], float("inf")
+    x, r = _rows(42, 9, d, dtype), _rows(43, 9, d, dtype)
+    bad = x.clone()
+    bad[2, d // 2], bad[5, 0], bad[7, d - 1] = inf, float("nan"), -inf
+    bad[8, 0], bad[8, d - 1] = inf, -inf
+    kw = {"residual": r.to(DEV)} if residual else {}
+    good = [0, 1, 3, 4, 6]
+    _, mean, rstd, *_ = seco.layer_norm_fwd(x.to(DEV), **kw)
+    _, m2, r2, *_ = seco.layer_norm_fwd(bad.to(DEV), **kw)
+    assert torch.equal(m2[good], mean[good]) and torch.equal(r2[good], rstd[good])
+    assert torch.isnan(r2[[2, 5, 7, 8]]).all()
+    assert m2[2] == inf and m2[7] == -inf and torch.isnan(m2[[5, 8]]).all()
+
+
+@pytest.mark.gpu
 def test_gain_types_missing_gain_and_wanted_sums():
     d, rows = 1000, 600
     x, dy = _rows(50, rows, d, torch.bfloat16), _rows(51, rows, d, torch.bfloat16)
