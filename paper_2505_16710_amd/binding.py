@@ -281,11 +281,11 @@ def layer_norm_fwd(x, gain=None, bias=None, eps=1e-5, residual=None, y=None, x_o
     return (_ext or _load_ext()).norm_fwd(x, gain, bias, eps, residual, y, x_out, stream)
 
 
-def layer_norm_bwd(x, gain, mean, rstd, d_y, d_in=None, d_x=None, with_gain=True, with_bias=True, ws=None, stream=None):
-    """Backward of layer_norm_fwd: (d_x, d_gain, d_bias), the last two [d] of the gain's dtype (of x's without a gain), None
-    where with_gain / with_bias is false.  x: what was normalised (x_out where there was a residual).  d_in (shape of x), if
+def layer_norm_bwd(x, gain, mean, rstd, d_y, d_in=None, d_x=None, with_gain=True, with_bias=True, ws=None, stream=None, dtype=None):
+    """Backward of layer_norm_fwd: (d_x, d_gain, d_bias), the last two [d] of the gain's dtype (without a gain of dtype, x's or
+    float32, default x's: a bias alone may be wider than the rows), None where with_gain / with_bias is false.  x: what was normalised (x_out where there was a residual).  d_in (shape of x), if
     given, is added to d_x: the gradient that reaches the rows past the norm.  d_x may be x, d_y or d_in."""
-    return (_ext or _load_ext()).norm_bwd(x, gain, mean, rstd, d_y, d_in, d_x, with_gain, with_bias, ws, stream)
+    return (_ext or _load_ext()).norm_bwd(x, gain, mean, rstd, d_y, d_in, d_x, with_gain, with_bias, ws, stream, dtype)
 
 
 def adamw_step(params, grads, m, v, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, masters=None, m_scales=None,

@@ -157,7 +157,7 @@ class LayerNorm(torch.autograd.Function):
     def forward(ctx, x, gain, bias=None, eps=1e-5, residual=None):
         y, mean, rstd, *out = _b.layer_norm_fwd(x, gain, bias, eps, residual)
         ctx.save_for_backward(out[0] if out else x, gain, mean, rstd)
-        ctx.has_residual, ctx.has_bias = residual is not None, bias is not None
+        ctx.has_residual, ctx.bias_type = residual is not None, None if bias is None else bias.dtype
         ctx.set_materialize_grads(False)
         return (y, out[0]) if out else y
 
@@ -169,7 +169,8 @@ class LayerNorm(torch.autograd.Function):
             return d_sum, None, None, None, d_sum if ctx.has_residual else None
         d_x, d_gain, d_bias = _b.layer_norm_bwd(x, gain, mean, rstd, d_y.contiguous(), None if d_sum is None else d_sum.contiguous(),
                                                 with_gain=gain is not None and ctx.needs_input_grad[1],
-                                                with_bias=ctx.has_bias and ctx.needs_input_grad[2])
+                                                with_bias=ctx.bias_type is not None and ctx.needs_input_grad[2],
+                                                dtype=ctx.bias_type if gain is None else None)
         return d_x, d_gain, d_bias, None, d_x if ctx.has_residual else None
 
 

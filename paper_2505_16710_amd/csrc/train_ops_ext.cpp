@@ -79,9 +79,15 @@ void vector_of(const Tensor& t, int64_t d, at::ScalarType type, const char* name
     throw Raised{};
   }
 }
-// the type of gain and bias (none: the rows')
-at::ScalarType gain_type(const Tensor& x, const Tensor* gain, const Tensor* bias) {
-  const at::ScalarType t = gain ? gain->scalar_type() : bias ? bias->scalar_type() : x.scalar_type();
+// the type of gain and bias (none: given, or the rows')
+at::ScalarType gain_type(const Tensor& x, const Tensor* gain, const Tensor* bias, PyObject* given = Py_None) {
+  at::ScalarType t = gain ? gain->scalar_type() : bias ? bias->scalar_type() : x.scalar_type();
+  if (given != Py_None) {
+    if (!THPDtype_Check(given)) raise(PyExc_TypeError, "dtype must be a torch dtype");
+    const at::ScalarType wanted = reinterpret_cast<THPDtype*>(given)->scalar_type;
+    if (gain && wanted != t) raise(PyExc_TypeError, "dtype: with a gain, its dtype");
+    t = wanted;
+  }
   if (t != x.scalar_type() && t != at::kFloat) raise(PyExc_TypeError, "gain and bias must have x's dtype or float32");
   return t;
 }
@@ -137,12 +143,12 @@ PyObject* norm_fwd(PyObject* const* a) {
   return Py_BuildValue("NNNN", out_ref(a[5], y), THPVariable_Wrap(mean), THPVariable_Wrap(rstd), out_ref(a[6], out));
 }
 
-// (x, gain, mean, rstd, d_y, d_in, d_x, with_gain, with_bias, ws, stream) -> (d_x, d_gain or None, d_bias or None)
+// (x, gain, mean, rstd, d_y, d_in, d_x, with_gain, with_bias, ws, stream, dtype or None) -> (d_x, d_gain or None, d_bias or None)
 PyObject* norm_bwd(PyObject* const* a) {
   const Tensor &x = tensor(a[0]), &mean = tensor(a[2]), &rstd = tensor(a[3]), &dy = tensor(a[4]);
   const Tensor *gain = opt_tensor(a[1]), *in = opt_tensor(a[5]), *dx_given = opt_tensor(a[6]), *ws_given = opt_tensor(a[9]);
   const Rows rows = rows_of(x, "x");
-  const at::ScalarType gt = gain_type(x, gain, nullptr);
+  const at::ScalarType gt = gain_type(x, gain, nullptr, a[11]);
   layer_norm_desc d = norm_desc(x, rows, gt);
   if (gain) vector_of(*gain, rows.d, gt, "gain");
   for (const Tensor* t : {&mean, &rstd})
@@ -546,6 +552,6 @@ PyObject* readout_axes(PyObject* const* a) {
 }  // namespace
 
 PyMethodDef train_methods[] = {SECO_METHOD("rotate_axes", rotate_axes, 6), SECO_METHOD("append_axes", append_axes, 10),
-                               SECO_METHOD("readout_axes", readout_axes, 12), SECO_METHOD("adamw", adamw, 15), SECO_METHOD("norm_fwd", norm_fwd, 8), SECO_METHOD("norm_bwd", norm_bwd, 11), {nullptr, nullptr, 0, nullptr}};
+                               SECO_METHOD("readout_axes", readout_axes, 12), SECO_METHOD("adamw", adamw, 15), SECO_METHOD("norm_fwd", norm_fwd, 8), SECO_METHOD("norm_bwd", norm_bwd, 12), {nullptr, nullptr, 0, nullptr}};
 
 }  // namespace seco_ext

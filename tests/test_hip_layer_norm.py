@@ -287,6 +287,34 @@ def test_gain_types_missing_gain_and_wanted_sums():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows", [700, 1500])
+def test_a_bias_without_a_gain_has_a_gradient_of_its_type(rows):
+    """An fp32 bias on bf16 rows: the sum over the rows in fp32, not rounded to bf16 on its way."""
+    from paper_2505_16710_amd.chunk_loop import LayerNorm
+    d = 96
+    x, dy = _rows(54, rows, d, torch.bfloat16), _rows(55, rows, d, torch.bfloat16)
+    bias = _rows(56, 1, d, torch.float32)[0].contiguous().to(DEV).requires_grad_()
+    LayerNorm.apply(x.to(DEV), None, bias).backward(dy.to(DEV))
+    bound = 64 * U * dy.double().abs().sum(0)
+    assert ((bias.grad.cpu().double() - dy.double().sum(0)).abs() <= bound).all()
+    _, mean, rstd = seco.layer_norm_fwd(x.to(DEV), None, bias.detach())
+    _, dg, db = seco.layer_norm_bwd(x.to(DEV), None, mean, rstd, dy.to(DEV), dtype=torch.float32)
+    assert dg.dtype == torch.float32 and torch.equal(db, bias.grad)
+    _, dg, db = seco.layer_norm_bwd(x.to(DEV), None, mean, rstd, dy.to(DEV))
+    assert dg.dtype == db.dtype == torch.bfloat16 and torch.equal(db, bias.grad.bfloat16())
+
+
+def test_refused_types_of_sums():
+    x, g, m = torch.zeros(4, 16), torch.ones(16), torch.zeros(4)
+    for args, dtype in (((x, g, m, m, x), torch.bfloat16), ((x, None, m, m, x), torch.bfloat16), ((x, None, m, m, x), torch.float16),
+                        ((x, None, m, m, x), 1)):
+        with pytest.raises(TypeError):
+            seco.layer_norm_bwd(*args, dtype=dtype)
+    with pytest.raises(ValueError, match="on one GPU"):
+        seco.layer_norm_bwd(x, g, m, m, x, dtype=torch.float32)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 1024, 4096])
 def test_layouts(d):
     """Leading dimensions, rows of a wider buffer, a row for all, unaligned starts."""
