@@ -315,7 +315,8 @@ int rope_rotate(const seco_desc* desc, int32_t n_heads, const void* x_in, void* 
  *   rope_readout_axes  and the gradients' way back: d_q (q_stride) turned back to d_q_out (o_stride; may be d_q),
  *                      d_k_new = R(-theta)(scaler * gk[rows]), d_v_new = scaler * gv[rows] for rows q_start + r of gk, gv (fp32,
  *                      g_stride), d_k_new and d_v_new with kv_stride
- * A pair of pointers (q and q_out, k_new and k_cache, ...) may be NULL (skipped).
+ * A pair of pointers (q and q_out, k_new and k_cache, ...) may be NULL (skipped).  A result may lie in the place of its pair's
+ * input, element for element; else results share no memory with what is read, nor with each other.
  */
 #define SECO_ROPE_MAX_AXES 4
 typedef struct rope_axes {
@@ -345,7 +346,8 @@ int rope_readout_axes(const seco_desc* desc, const rope_axes* axes, const void* 
  * gain, bias   [d] of gain_dtype, or NULL (ones, zeros)
  * mean, rstd   fp32 [rows], one behind the other
  * residual and x_out go together, both or neither; x_out may be x or residual, y may be x when there is no residual (same
- * stride).  d_in may be NULL (nothing is added); d_x may be x, d_y or d_in (same stride).  In the backward, x is the row that
+ * stride).  Else results share no memory with what is read, nor with each other.  d_in may be NULL (nothing is added); d_x may be
+ * x, d_y or d_in (same stride).  In the backward, x is the row that
  * was normalised: x_out where there was a residual.  d_gain, d_bias: overwritten; NULL: not wanted.
  * rows = 0 is allowed (d_gain and d_bias are then zeros).  Row strides of inputs may be 0 (one row for all).
  * ws of the backward: layer_norm_workspace_bytes(desc) bytes, 16-byte aligned; not needed (NULL) where these are 0, or when

@@ -18,9 +18,82 @@ struct OnGpu {
   void* s;
   OnGpu(const Tensor& t, PyObject* o) : guard(t.device()), s(o == Py_None ? c10::hip::getCurrentHIPStream(t.device().index()).stream() : stream(o)) {}
 };
-// a result in the place of an input lies there element for element
-void in_place_or_apart(const Tensor& out, const Tensor& in, const char* name) {
-  if (out.data_ptr() != in.data_ptr() || out.numel() == 0) return;
+// Where a tensor's elements lie, of a buffer [B, H, N, D] those of rows [row, row + rows): all in [at, end)
+struct Spread {
+  uintptr_t at, end;
+  const Tensor& t;
+  int64_t rows;
+  explicit Spread(const Tensor& t, int64_t row = 0, int64_t rows = -1) : t(t), rows(rows) {
+    const int64_t e = t.element_size();
+    at = reinterpret_cast<uintptr_t>(t.data_ptr()) + (uintptr_t)(rows < 0 ? 0 : row * t.stride(2) * e);
+    end = at + (uintptr_t)e;
+    for (int64_t i = 0; i < t.dim(); ++i) {
+      if (size(i) == 0) {                        // nothing lies anywhere
+        end = at;
+        return;
+      }
+      end += (uintptr_t)((size(i) - 1) * t.stride(i) * e);
+    }
+  }
+  int64_t size(int64_t i) const { return i == 2 && rows >= 0 ? rows : t.size(i); }
+};
+// The distances of two tensors' elements: sums of stride * i with first <= i <= last for every stride, and of pieces without
+// gaps `width` bytes behind each.  Elements meet if such a sum comes to lie in a range.
+struct Distances {
+  struct Term {
+    int64_t stride, first, last;
+  };
+  c10::SmallVector<Term, 8> terms;
+  int budget = 1000;                             // sums looked at
+  // the tensor's dimensions by their strides; those that leave no gap make a piece
+  int64_t add(const Spread& x, int sign) {
+    c10::SmallVector<std::pair<int64_t, int64_t>, 8> dims;
+    for (int64_t i = 0; i < x.t.dim(); ++i)
+      if (x.size(i) > 1) dims.emplace_back(x.t.stride(i) * (int64_t)x.t.element_size(), x.size(i) - 1);
+    std::sort(dims.begin(), dims.end());
+    int64_t width = x.t.element_size();
+    size_t i = 0;
+    for (; i < dims.size() && dims[i].first <= width; ++i) width += dims[i].first * dims[i].second;
+    for (; i < dims.size(); ++i) {
+      const auto [stride, last] = dims[i];
+      auto* at = std::find_if(terms.begin(), terms.end(), [&](const Term& t) { return t.stride == stride; });
+      if (at == terms.end()) at = terms.insert(at, Term{stride, 0, 0});
+      (sign > 0 ? at->last : at->first) += sign * last;
+    }
+    return width;
+  }
+  // whether a sum over the terms from the k-th on (largest strides first) lies in [low, high]; not, if the budget is used up
+  bool reach(size_t k, int64_t low, int64_t high) {
+    if (k == terms.size()) return low <= 0 && 0 <= high;
+    int64_t least = 0, most = 0;                 // of what follows
+    for (size_t i = k + 1; i < terms.size(); ++i) least += terms[i].stride * terms[i].first, most += terms[i].stride * terms[i].last;
+    const Term& t = terms[k];
+    auto down = [](int64_t a, int64_t b) { return a / b - (a % b < 0); };
+    const int64_t first = std::max(t.first, -down(most - low, t.stride)), last = std::min(t.last, down(high - least, t.stride));
+    for (int64_t i = first; i <= last && --budget >= 0; ++i)
+      if (reach(k + 1, low - i * t.stride, high - i * t.stride)) return true;
+    return false;
+  }
+};
+// Whether two tensors share memory: their ranges first, then, where these meet (columns of one buffer), their elements.  Layouts that
+// would take long to tell apart count as apart.
+bool share(const Spread& a, const Spread& b) {
+  if (a.end <= b.at || b.end <= a.at || a.at == a.end || b.at == b.end) return false;
+  Distances x;
+  const int64_t wide_a = x.add(a, 1), wide_b = x.add(b, -1), off = (int64_t)(a.at - b.at);
+  std::sort(x.terms.begin(), x.terms.end(), [](const auto& p, const auto& q) { return p.stride > q.stride; });
+  return x.reach(0, 1 - wide_a - off, wide_b - 1 - off);
+}
+void need_apart(const Spread& a, const Spread& b, const char* name, const char* other) {
+  if (!share(a, b)) return;
+  PyErr_Format(PyExc_ValueError, "%s overlaps %s", name, other);
+  throw Raised{};
+}
+// a result in the place of an input lies there element for element; else it shares nothing with it, since other workgroups may
+// have yet to read what one has written
+void in_place_or_apart(const Tensor& out, const Tensor& in, const char* name, const char* other) {
+  if (out.numel() == 0) return;
+  if (out.data_ptr() != in.data_ptr()) return need_apart(Spread(out), Spread(in), name, other);
   for (int64_t i = 0; i < in.dim(); ++i)
     if (in.size(i) > 1 && out.stride(i) != in.stride(i)) {
       PyErr_Format(PyExc_ValueError, "%s: in the place of an input it needs that one's strides", name);
@@ -123,9 +196,10 @@ PyObject* norm_fwd(PyObject* const* a) {
     if (t) {
       const char* name = t == y_given ? "y" : "x_out";
       rows_like(*t, x, name);
-      in_place_or_apart(*t, x, name);
-      if (res) in_place_or_apart(*t, *res, name);
+      in_place_or_apart(*t, x, name, "x");
+      if (res) in_place_or_apart(*t, *res, name, "residual");
     }
+  if (y_given && out_given) need_apart(Spread(*y_given), Spread(*out_given), "y", "x_out");
   for (const Tensor* t : {&x, gain, bias, res, y_given, out_given})
     if (t) same_gpu(x, *t);
   OnGpu on(x, a[7]);
@@ -159,7 +233,7 @@ PyObject* norm_bwd(PyObject* const* a) {
   if (dx_given) {
     rows_like(*dx_given, x, "d_x");
     for (const Tensor* t : {&x, &dy, in})
-      if (t) in_place_or_apart(*dx_given, *t, "d_x");
+      if (t) in_place_or_apart(*dx_given, *t, "d_x", t == &x ? "x" : t == &dy ? "d_y" : "d_in");
   }
   for (const Tensor* t : {&mean, &rstd, &dy, gain, in, dx_given, ws_given})
     if (t) same_gpu(x, *t);
@@ -378,6 +452,13 @@ void writable(const Tensor& t, const char* name) {
       throw Raised{};
     }
 }
+// whether a tensor lies element for element where those rows of a buffer do
+bool in_place(const Spread& rows, const Tensor& t) {
+  if (rows.at != reinterpret_cast<uintptr_t>(t.data_ptr()) || rows.t.scalar_type() != t.scalar_type()) return false;
+  for (int i = 0; i < 4; ++i)
+    if (t.size(i) > 1 && t.stride(i) != rows.t.stride(i)) return false;
+  return true;
+}
 // a dimension of one element may have any stride; the library asks for one that keeps rows on their boundaries
 void heads_strides(const Tensor& t, int64_t out[3]) {
   for (int i = 0; i < 3; ++i) out[i] = t.size(i) == 1 ? (i == 2 ? t.size(3) : 0) : t.stride(i);
@@ -419,7 +500,7 @@ PyObject* rotate_axes(PyObject* const* a) {
     heads_tensor(o, "out", B, C, D, x.scalar_type());
     writable(o, "out");
     if (o.size(1) != x.size(1)) raise(PyExc_ValueError, "out must have the shape of x");
-    in_place_or_apart(o, x, "out");
+    in_place_or_apart(o, x, "out", "x");
     same_gpu(x, o);
   }
   same_gpu(x, pos);
@@ -458,11 +539,22 @@ PyObject* append_axes(PyObject* const* a) {
     heads_tensor(o, "q_out", B, C, D, kn.scalar_type());
     writable(o, "q_out");
     if (!q || o.size(1) != q->size(1)) raise(PyExc_ValueError, "q_out must have the shape of q");
-    in_place_or_apart(o, *q, "q_out");
+    in_place_or_apart(o, *q, "q_out", "q");
+    need_apart(Spread(o), Spread(kn), "q_out", "k_new");
+    need_apart(Spread(o), Spread(vn), "q_out", "v_new");
     same_gpu(kn, o);
   }
   for (const Tensor* t : {&vn, &kc, &vc, &pos, q})
     if (t) same_gpu(kn, *t);
+  const Spread k_rows(kc, row, C), v_rows(vc, row, C);          // what is written; keys and values may be there already
+  need_apart(k_rows, v_rows, "k_cache", "v_cache");
+  for (const Spread* rows : {&k_rows, &v_rows}) {
+    const char* name = rows == &k_rows ? "k_cache" : "v_cache";
+    if (q) need_apart(*rows, Spread(*q), name, "q");
+    if (a[8] != Py_None) need_apart(*rows, Spread(tensor(a[8])), name, "q_out");
+    for (const Tensor* t : {&kn, &vn})
+      if ((rows == &k_rows) != (t == &kn) || !in_place(*rows, *t)) need_apart(*rows, Spread(*t), name, t == &kn ? "k_new" : "v_new");
+  }
   OnGpu on(kn, a[9]);
   Tensor out;
   if (q) out = a[8] == Py_None ? fresh_like(*q) : tensor(a[8]);
@@ -519,11 +611,27 @@ PyObject* readout_axes(PyObject* const* a) {
     heads_tensor(o, "dq_out", B, C, D, type);
     writable(o, "dq_out");
     if (!dq || o.size(1) != dq->size(1)) raise(PyExc_ValueError, "dq_out must have the shape of d_q");
-    in_place_or_apart(o, *dq, "dq_out");
+    in_place_or_apart(o, *dq, "dq_out", "d_q");
     same_gpu(gk, o);
   }
   for (const Tensor* t : {&gv, &pos, dq, dk_given, dv_given})
     if (t) same_gpu(gk, *t);
+  const Spread gk_rows(gk, row, C), gv_rows(gv, row, C);
+  auto results = [&](const Tensor* t, const char* name, const Spread* own) {      // own: what t may lie in the place of
+    if (!t) return;
+    if (own != &gk_rows || !in_place(gk_rows, *t)) need_apart(Spread(*t), gk_rows, name, "gk");
+    if (own != &gv_rows || !in_place(gv_rows, *t)) need_apart(Spread(*t), gv_rows, name, "gv");
+  };
+  const Tensor* dq_given = opt_tensor(a[7]);
+  results(dq_given, "dq_out", nullptr);
+  results(dk_given, "d_k", &gk_rows);
+  results(dv_given, "d_v", &gv_rows);
+  if (dk_given) {
+    need_apart(Spread(*dk_given), Spread(*dv_given), "d_k", "d_v");
+    for (const Tensor* t : {dk_given, dv_given})
+      for (const Tensor* other : {dq, dq_given})
+        if (other) need_apart(Spread(*t), Spread(*other), t == dk_given ? "d_k" : "d_v", other == dq ? "d_q" : "dq_out");
+  }
   OnGpu on(gk, a[11]);
   Tensor out, dk, dv;
   if (dq) out = a[7] == Py_None ? fresh_like(*dq) : tensor(a[7]);

@@ -509,6 +509,35 @@ def test_refusals():
             call()
 
 
+def test_results_that_overlap_are_refused():
+    """Two results in one place, rows that another row's workgroup may have overwritten; beside each other they may lie."""
+    m, flat = torch.zeros(4), torch.zeros(400)
+    buf = flat[:320].view(5, 64)
+    x, next_row, beside, across = buf[:4, :16], buf[1:, :16], buf[:4, 16:32], buf[:4, 8:24]
+    apart = torch.zeros(4, 16)
+    fwd = seco.layer_norm_fwd
+
+    def bwd(x, dy, **kw):
+        seco.layer_norm_bwd(x, None, m, m, dy, **kw)
+    for call in (lambda: fwd(x, residual=apart, y=beside, x_out=beside), lambda: fwd(x, residual=apart, y=x, x_out=x),
+                 lambda: fwd(x, residual=apart, y=beside, x_out=buf[:4, 24:40]), lambda: fwd(x, y=next_row), lambda: fwd(x, y=across),
+                 lambda: fwd(apart, residual=x, x_out=next_row), lambda: fwd(flat[:64].view(4, 16), y=flat[4:68].view(4, 16)),
+                 lambda: fwd(x[:1].expand(4, 16), y=flat[4:68].view(4, 16)), lambda: bwd(x, apart, d_x=next_row),
+                 lambda: bwd(next_row, apart, d_x=x), lambda: bwd(apart, x, d_x=across), lambda: bwd(apart, apart, d_in=x, d_x=next_row),
+                 lambda: bwd(flat[8:72].view(4, 16), apart, d_x=flat[:256].view(4, 64)[:, :16])):
+        with pytest.raises(ValueError, match="overlaps"):
+            call()
+    rows3 = torch.zeros(2, 5, 3, 16)
+    for call in (lambda: fwd(x, y=beside), lambda: fwd(x, residual=apart, y=beside, x_out=x), lambda: fwd(x, residual=beside, x_out=beside),
+                 lambda: fwd(flat[:64].view(4, 16), y=flat[64:128].view(4, 16)), lambda: fwd(buf[:2, :16], y=buf[2:4, :16]),
+                 lambda: fwd(flat[:320].view(10, 32)[::2, :16], y=flat[:320].view(10, 32)[1::2, :16]),
+                 lambda: fwd(flat[:320].view(5, 4, 16)[:, 0], y=flat[:320].view(10, 2, 16)[:5, 1]),
+                 lambda: fwd(rows3[..., 0, :], y=rows3[..., 1, :]), lambda: bwd(x, apart, d_x=x), lambda: bwd(x, beside, d_x=beside),
+                 lambda: bwd(x, apart, d_in=beside, d_x=beside), lambda: bwd(x, apart, d_x=beside), lambda: bwd(x, x, d_x=x)):
+        with pytest.raises(ValueError, match="on one GPU"):
+            call()
+
+
 def test_status_codes():
     import ctypes as C
     lib = seco.load_library()

@@ -341,6 +341,98 @@ def test_refusals():
             call()
 
 
+def test_results_that_overlap_are_refused():
+    """Layouts drawn at random over one buffer, compared element by element: a result that shares some with the input is refused
+    unless it lies in its place, and no other one is."""
+    axes, room = seco.RopeAxes((2, 2), BASE), torch.zeros(4000)
+    g = torch.Generator().manual_seed(5)
+
+    def draw(n):
+        return int(torch.randint(0, n, (1,), generator=g))
+    numbers, seen = torch.arange(4000), {True: 0, False: 0}
+    for _ in range(600):
+        B, H, C = 1 + draw(3), 1 + draw(3), 1 + draw(4)
+        pos, pair = torch.zeros(2, 1, C, dtype=torch.int64), []
+        strides = None
+        for _ in range(2):
+            order = [(0, 1, 2), (0, 2, 1), (1, 0, 2), (2, 0, 1)][draw(4)]           # from the outermost dimension in
+            if strides is None or draw(3) == 0:
+                strides, step = [0, 0, 0, 1], 8 + 8 * draw(3) * draw(2)
+                for i in reversed(order):
+                    strides[i] = step
+                    step *= (B, H, C)[i] + draw(2) * draw(3)
+            pair.append((strides, 8 * draw(40) if draw(2) else draw(60)))
+        if max(st[0] * B + st[1] * H + st[2] * C + off + 8 for st, off in pair) > 4000:
+            continue
+        x, out = (torch.as_strided(room, (B, H, C, 8), st, off) for st, off in pair)
+        used = [set(torch.as_strided(numbers, (B, H, C, 8), st, off).flatten().tolist()) for st, off in pair]
+        if pair[0][1] == pair[1][1]:
+            same = all(n == 1 or a == b for n, a, b in zip((B, H, C), pair[0][0], pair[1][0]))
+            want = "on one GPU" if same else "strides"
+        else:
+            want = "overlaps" if used[0] & used[1] else "on one GPU"
+            seen[want == "overlaps"] += 1
+        with pytest.raises(ValueError, match=want):
+            seco.rope_rotate_axes(x, pos, axes, out=out)
+    assert min(seen.values()) > 100
+    joint = torch.zeros(1, 12, 6 * 8)
+    q, k, v = (joint[..., a:b].unflatten(2, (-1, 8)).transpose(1, 2) for a, b in ((0, 16), (16, 32), (32, 48)))
+    cache = torch.zeros(1, 2, 20, 8)
+    pos = torch.zeros(2, 1, 10, dtype=torch.int64)
+    q, k, v = (t[:, :, :10] for t in (q, k, v))
+    for bad in (k, v, joint[:, 2:, :16].unflatten(2, (-1, 8)).transpose(1, 2), joint[:, :10, 8:24].unflatten(2, (-1, 8)).transpose(1, 2)):
+        with pytest.raises(ValueError, match="overlaps"):
+            seco.rope_append_axes(q, k, v, cache, cache.clone(), 4, pos, axes, q_out=bad)
+    with pytest.raises(ValueError, match="overlaps"):
+        seco.rope_readout_axes(q, cache, cache, 4, pos, axes, dq_out=joint[:, 2:, :16].unflatten(2, (-1, 8)).transpose(1, 2))
+
+
+@pytest.mark.gpu
+def test_caches_and_results_that_share_memory():
+    """Keys and values in one tensor, halves of it or rows in turn; a projection that lies in the cache already; one place for both
+    is refused."""
+    axes, B, H, C, D, N = seco.RopeAxes((32, 32), BASE), 2, 3, 10, 128, 40
+    kn, vn = (_rows(k, B, H, C, D, dtype=torch.bfloat16).to(DEV) for k in (1, 2))
+    pos = _positions(3, 2, B, C).to(DEV)
+    kc, vc = (torch.zeros(B, H, N, D, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    seco.rope_append_axes(None, kn, vn, kc, vc, 7, pos, axes)
+    for shape, at in (((2, B, H, N, D), 0), ((B, 2, H, N, D), 1), ((B, H, 2, N, D), 2), ((B, H, N, 2, D), 3), ((B, H, N, D, 2), None)):
+        both = torch.zeros(*shape, dtype=torch.bfloat16, device=DEV)
+        if at is None:                                       # (elements in turn: no head_dim is contiguous)
+            with pytest.raises(ValueError, match="head_dim"):
+                seco.rope_append_axes(None, kn, vn, both[..., 0], both[..., 1], 7, pos, axes)
+            continue
+        k, v = both.unbind(at)
+        seco.rope_append_axes(None, kn, vn, k, v, 7, pos, axes)
+        assert torch.equal(k, kc) and torch.equal(v, vc)
+    there = [torch.zeros(B, H, N, D, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    for t, new in zip(there, (kn, vn)):
+        t[:, :, 7:17] = new
+    seco.rope_append_axes(None, there[0][:, :, 7:17], there[1][:, :, 7:17], *there, 7, pos, axes)
+    assert torch.equal(there[0], kc) and torch.equal(there[1], vc)
+    for bad in ((kc, kc), (kc[:, :2], kc[:, 1:])):
+        with pytest.raises(ValueError, match="overlaps"):
+            seco.rope_append_axes(None, kn[:, :bad[0].shape[1]], vn[:, :bad[0].shape[1]], *bad, 7, pos, axes)
+    spare = torch.zeros_like(kc)[:, :, :C]
+    for args in ((kc[:, :, 8:18], spare), (vc[:, :, 7:17], spare), (spare, kc[:, :, 16:26])):
+        with pytest.raises(ValueError, match="overlaps"):
+            seco.rope_append_axes(None, *args, kc, vc, 7, pos, axes)
+    with pytest.raises(ValueError, match="overlaps"):
+        seco.rope_append_axes(kc[:, :, 7:17], kn, vn, kc, vc, 7, pos, axes)
+    with pytest.raises(ValueError, match="overlaps"):
+        seco.rope_append_axes(kn, kn, vn, kc, vc, 7, pos, axes, q_out=kc[:, :, 3:13])
+    g = torch.randn(B, H, N, D, device=DEV)
+    for kw in (dict(d_k=kn, d_v=kn), dict(d_k=kn, d_v=vn, dq_out=kn)):
+        with pytest.raises(ValueError, match="overlaps"):
+            seco.rope_readout_axes(kn.clone(), g, g, 7, pos, axes, **kw)
+    with pytest.raises(ValueError, match="overlaps"):
+        seco.rope_readout_axes(None, g, g, 7, pos, axes, d_k=g[:, :, 8:18], d_v=torch.zeros_like(g)[:, :, :C])
+    want = seco.rope_readout_axes(None, g, 2 * g, 7, pos, axes, dtype=torch.float32)
+    gk, gv = g.clone(), 2 * g
+    seco.rope_readout_axes(None, gk, gv, 7, pos, axes, d_k=gk[:, :, 7:17], d_v=gv[:, :, 7:17])
+    assert torch.equal(gk[:, :, 7:17], want[1]) and torch.equal(gv[:, :, 7:17], want[2]) and torch.equal(gk[:, :, 17:], g[:, :, 17:])
+
+
 def test_status_codes():
     lib = seco.load_library()
     from paper_2505_16710_amd.binding import SecoDesc
