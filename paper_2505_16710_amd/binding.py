@@ -263,13 +263,15 @@ def rope_rotate_axes(x, positions, axes, inverse=False, out=None, stream=None):
 
 def rope_append_axes(q, k_new, v_new, k_cache, v_cache, row_begin, positions, axes, q_out=None, stream=None):
     """One launch from the projections to the attention: queries [B, Hq, C, D] (or None) turned, returned; keys [B, Hkv, C, D]
-    turned and values copied to cache rows [row_begin, row_begin + C).  q_out may be q."""
+    turned and values copied to cache rows [row_begin, row_begin + C).  q_out may be q.  Keys and values that lie in other strides
+    than each other, or whose caches do, take two launches."""
     return (_ext or _load_ext()).append_axes(q, k_new, v_new, k_cache, v_cache, row_begin, positions, axes.packed, q_out, stream)
 
 
 def rope_readout_axes(d_q, gk, gv, row_begin, positions, axes, scaler=1.0, dq_out=None, d_k=None, d_v=None, dtype=None, stream=None):
     """The gradients' way back, one launch: (d_q turned back or None, d_k, d_v) with d_k, d_v = scaler * (gk turned back, gv)
-    for buffer rows [row_begin, row_begin + C), C the positions' rows, in d_q's dtype (without d_q: dtype).  dq_out may be d_q."""
+    for buffer rows [row_begin, row_begin + C), C the positions' rows, in d_q's dtype (without d_q: dtype).  dq_out may be d_q.
+    Two launches where gk and gv, or d_k and d_v, lie in other strides than each other."""
     return (_ext or _load_ext()).readout_axes(d_q, gk, gv, row_begin, positions, axes.packed, scaler, dq_out, d_k, d_v, dtype, stream)
 
 

@@ -429,10 +429,10 @@ void heads_tensor(const Tensor& t, const char* name, int64_t B, int64_t rows, in
                (long long)B, (long long)rows, (long long)D);
   throw Raised{};
 }
-// k / v or their like: one shape, one set of strides
+// k / v or their like: one shape and type
 void like_each_other(const Tensor& a, const Tensor& b, const char* names) {
-  if (a.sizes() == b.sizes() && a.strides() == b.strides() && a.scalar_type() == b.scalar_type()) return;
-  PyErr_Format(PyExc_ValueError, "%s must share shape, strides and dtype", names);
+  if (a.sizes() == b.sizes() && a.scalar_type() == b.scalar_type()) return;
+  PyErr_Format(PyExc_ValueError, "%s must share shape and dtype", names);
   throw Raised{};
 }
 // rows [begin, begin + n) of a cache or gradient buffer [B, H, N, D]
@@ -462,6 +462,23 @@ bool in_place(const Spread& rows, const Tensor& t) {
 // a dimension of one element may have any stride; the library asks for one that keeps rows on their boundaries
 void heads_strides(const Tensor& t, int64_t out[3]) {
   for (int i = 0; i < 3; ++i) out[i] = t.size(i) == 1 ? (i == 2 ? t.size(3) : 0) : t.stride(i);
+}
+// The library's calls take keys and values in one layout; where theirs differ, values take a call of their own.
+bool one_layout(const Tensor& a, const Tensor& b) {
+  for (int64_t i = 0; i < a.dim(); ++i)
+    if (a.size(i) > 1 && a.stride(i) != b.stride(i)) return false;
+  return true;
+}
+// ... of which nothing may be refused once the first is on its way: what the library asks of rows and their distances
+void rows_aligned(const Tensor& t, const char* where) {
+  int64_t st[3];
+  heads_strides(t, st);
+  const int64_t e = t.element_size();
+  for (int i = 0; i < 3; ++i) {
+    if (st[i] > (int64_t)1 << (i == 2 ? 30 : 40)) check(SECO_ERR_TOO_LARGE, where);
+    if (st[i] * e % 16) check(SECO_ERR_ALIGN, where);
+  }
+  if (st[2] < t.size(3) || reinterpret_cast<uintptr_t>(t.data_ptr()) % 16) check(SECO_ERR_ALIGN, where);
 }
 seco_desc axes_desc(int64_t B, int64_t rows, int64_t D, at::ScalarType type, int64_t row_begin, const char* where) {
   if (B > 65535 || rows > 1 << 27 || D > 256 || row_begin > (int64_t)1 << 30) check(SECO_ERR_TOO_LARGE, where);
@@ -528,8 +545,11 @@ PyObject* append_axes(PyObject* const* a) {
   fits_axes(axes, D);
   like_each_other(kn, vn, "k_new and v_new");
   like_each_other(kc, vc, "k_cache and v_cache");
+  heads_tensor(vn, "v_new", B, C, D, kn.scalar_type());
   rows_inside(kc, "k_cache", B, Hkv, D, row, C, kn.scalar_type());
+  rows_inside(vc, "v_cache", B, Hkv, D, row, C, kn.scalar_type());
   writable(kc, "k_cache");
+  writable(vc, "v_cache");
   if (q) heads_tensor(*q, "q", B, C, D, kn.scalar_type());
   seco_desc d = axes_desc(B, C, D, kn.scalar_type(), row, "rope_append_axes");
   int64_t ps[3];
@@ -566,9 +586,19 @@ PyObject* append_axes(PyObject* const* a) {
     heads_strides(*q, d.q_stride);
     heads_strides(out, d.o_stride);
   }
-  if (kn.numel() > 0)
-    check(lib.rope_append_axes(&d, &axes.x, ptr(q), q ? ptr(out) : nullptr, ptr(kn), ptr(vn), ptr(kc), ptr(vc),
-                               static_cast<const int64_t*>(ptr(pos)), ps, on.s), "rope_append_axes");
+  const int64_t* at = static_cast<const int64_t*>(ptr(pos));
+  if (kn.numel() > 0) {
+    const bool both = one_layout(kn, vn) && one_layout(kc, vc);
+    for (const Tensor* t : {&vn, &vc})
+      if (!both) rows_aligned(*t, "rope_append_axes");
+    check(lib.rope_append_axes(&d, &axes.x, ptr(q), q ? ptr(out) : nullptr, ptr(kn), both ? ptr(vn) : nullptr, ptr(kc), both ? ptr(vc) : nullptr,
+                               at, ps, on.s), "rope_append_axes");
+    if (!both) {
+      heads_strides(vn, d.g_stride);
+      heads_strides(vc, d.kv_stride);
+      check(lib.rope_append_axes(&d, &axes.x, nullptr, nullptr, nullptr, ptr(vn), nullptr, ptr(vc), at, ps, on.s), "rope_append_axes");
+    }
+  }
   if (!q) Py_RETURN_NONE;
   return out_ref(a[8], out);
 }
@@ -594,13 +624,16 @@ PyObject* readout_axes(PyObject* const* a) {
   like_each_other(gk, gv, "gk and gv");
   if (Hkv < 1) raise(PyExc_ValueError, "gk: expected at least one head");
   rows_inside(gk, "gk", B, Hkv, D, row, C, at::kFloat);
+  rows_inside(gv, "gv", B, Hkv, D, row, C, at::kFloat);
   fits_axes(axes, D);
   if (dq) heads_tensor(*dq, "d_q", B, C, D, type);
   if ((dk_given == nullptr) != (dv_given == nullptr)) raise(PyExc_ValueError, "d_k and d_v go together");
   if (dk_given) {
     like_each_other(*dk_given, *dv_given, "d_k and d_v");
     heads_tensor(*dk_given, "d_k", B, C, D, type);
+    heads_tensor(*dv_given, "d_v", B, C, D, type);
     writable(*dk_given, "d_k");
+    writable(*dv_given, "d_v");
     if (dk_given->size(1) != Hkv) raise(PyExc_ValueError, "d_k must have the heads of gk");
   }
   seco_desc d = axes_desc(B, C, D, type, row, "rope_readout_axes");
@@ -650,9 +683,20 @@ PyObject* readout_axes(PyObject* const* a) {
     heads_strides(*dq, d.q_stride);
     heads_strides(out, d.o_stride);
   }
-  if (dk.numel() > 0)
-    check(lib.rope_readout_axes(&d, &axes.x, ptr(dq), dq ? ptr(out) : nullptr, fptr(gk), fptr(gv), ptr(dk), ptr(dv), (float)real(a[6]),
-                                static_cast<const int64_t*>(ptr(pos)), ps, on.s), "rope_readout_axes");
+  const int64_t* at = static_cast<const int64_t*>(ptr(pos));
+  const float scaler = (float)real(a[6]);
+  if (dk.numel() > 0) {
+    const bool both = one_layout(gk, gv) && one_layout(dk, dv);
+    for (const Tensor* t : {&gv, (const Tensor*)&dv})
+      if (!both) rows_aligned(*t, "rope_readout_axes");
+    check(lib.rope_readout_axes(&d, &axes.x, ptr(dq), dq ? ptr(out) : nullptr, fptr(gk), both ? fptr(gv) : nullptr, ptr(dk), both ? ptr(dv) : nullptr,
+                                scaler, at, ps, on.s), "rope_readout_axes");
+    if (!both) {
+      heads_strides(gv, d.g_stride);
+      heads_strides(dv, d.kv_stride);
+      check(lib.rope_readout_axes(&d, &axes.x, nullptr, nullptr, nullptr, fptr(gv), nullptr, ptr(dv), scaler, at, ps, on.s), "rope_readout_axes");
+    }
+  }
   PyObject* first = dq ? out_ref(a[7], out) : (Py_INCREF(Py_None), Py_None);
   return Py_BuildValue("NNN", first, out_ref(a[8], dk), out_ref(a[9], dv));
 }

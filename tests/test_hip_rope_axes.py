@@ -383,8 +383,45 @@ def test_results_that_overlap_are_refused():
     for bad in (k, v, joint[:, 2:, :16].unflatten(2, (-1, 8)).transpose(1, 2), joint[:, :10, 8:24].unflatten(2, (-1, 8)).transpose(1, 2)):
         with pytest.raises(ValueError, match="overlaps"):
             seco.rope_append_axes(q, k, v, cache, cache.clone(), 4, pos, axes, q_out=bad)
+    for kw in (dict(k=k[..., ::2]), dict(v=torch.zeros(1, 2, 8, 10).transpose(2, 3)), dict(vc=cache.transpose(2, 3).contiguous().transpose(2, 3)),
+               dict(vc=cache[:, :, :1].expand(1, 2, 20, 8))):
+        with pytest.raises(ValueError, match="head_dim|expanded"):
+            seco.rope_append_axes(None, kw.get("k", k), kw.get("v", v), cache, kw.get("vc", cache.clone()), 4, pos, axes)
     with pytest.raises(ValueError, match="overlaps"):
         seco.rope_readout_axes(q, cache, cache, 4, pos, axes, dq_out=joint[:, 2:, :16].unflatten(2, (-1, 8)).transpose(1, 2))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("t,C", [("bf16", 10), ("f32", 1)])
+def test_keys_and_values_in_layouts_of_their_own(t, C):
+    """Keys that a norm has made contiguous beside values in the joint projection; caches, gradient buffers and results likewise."""
+    axes, B, Hq, H, D, N, dtype = seco.RopeAxes((32, 32), BASE), 2, 4, 2, 128, 40, TYPES[t]
+    joint = _rows(1, B, C, (Hq + 2 * H) * D, dtype=dtype).to(DEV)
+    q, k, v = (x.unflatten(2, (-1, D)).transpose(1, 2) for x in joint.split((Hq * D, H * D, H * D), 2))
+    pos = _positions(3, 2, B, C).to(DEV)
+
+    def caches(kind):
+        a = torch.zeros(B, H, N, D, dtype=dtype, device=DEV)
+        return a, (torch.zeros(B, N, H, D, dtype=dtype, device=DEV).transpose(1, 2) if kind else a.clone())
+    want = caches(0)
+    out = seco.rope_append_axes(q, k, v, *want, 7, pos, axes)
+    for kn, vn, kind in ((k.contiguous(), v, 0), (k, v.contiguous(), 0), (k, v, 1), (k.contiguous(), v, 1)):
+        got = caches(kind)
+        assert torch.equal(seco.rope_append_axes(q, kn, vn, *got, 7, pos, axes), out)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    gk, gv = (torch.randn(B, H, N, D, device=DEV) for _ in range(2))
+    want = seco.rope_readout_axes(q, gk, gv, 7, pos, axes, scaler=1.5)
+    rows = gv.transpose(1, 2).contiguous().transpose(1, 2)
+    for ga, gb, kw in ((gk, rows, {}), (gk, gv, dict(d_k=torch.empty_like(k.contiguous()), d_v=v)), (gk, rows, dict(d_k=k, d_v=v))):
+        got = seco.rope_readout_axes(q, ga, gb, 7, pos, axes, scaler=1.5, **kw)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    # what the values' own launch would refuse is refused in front of both
+    flat = torch.zeros(B * H * C * D + 8, dtype=dtype, device=DEV)
+    for odd in (flat[1:1 + B * H * C * D].view(B, H, C, D), torch.zeros(B, H, C, D + 1, dtype=dtype, device=DEV)[..., :D]):
+        got = caches(1)
+        with pytest.raises(seco.SecoError):
+            seco.rope_append_axes(q, k, odd, *got, 7, pos, axes)
+        assert not got[0].any() and not got[1].any()
 
 
 @pytest.mark.gpu
