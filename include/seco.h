@@ -387,7 +387,9 @@ size_t layer_norm_workspace_bytes(const layer_norm_desc* desc);
  *   step          device, two int64: [0] steps taken so far, read and incremented by the call (so that a captured graph
  *                 counts on when it is replayed); [1] the call's own, 0 before and after every call
  *   lr_device, grad_scale_device   device fp32, or NULL: read when the kernels run; lr_device replaces lr
- * A gradient that is not finite makes its element of p NaN, and of the states what that element alone would be.
+ * A gradient that is not finite makes its element of p NaN, and of the states what that element alone would be.  e4m3 has no
+ * infinity: with state_bits 8 an m or sqrt(v) that overflows (a square does from gradients of 1.8e19 on) is stored as NaN, and
+ * the element of p is NaN from the next step on; with 32 it stays infinite, and with v the element of p where it is.
  * Errors: SECO_ERR_RANGE for lr, eps, weight_decay not finite or negative and betas outside [0, 1); SECO_ERR_DTYPE for
  * state_bits or a dtype that is none, and for a master of an fp32 parameter.
  */

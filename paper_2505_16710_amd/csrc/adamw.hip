@@ -7,7 +7,7 @@
 // largest magnitude / 448.  That unit is no power of two, so that the largest element is kept to fp32: a block whose squares all
 // decay by b2 = 0.999 a step keeps its codes and follows in its unit, while a single code could not move by so little.  r instead
 // of v: its three bits and 18 powers of two of range then hold v over 36.  An r that is not zero is never stored as
-// zero (its m / eps would be unbounded), but as at least the smallest code.  The update itself uses m and v before they are rounded.
+// zero (its m / eps would be unbounded), but as at least the smallest code; an infinite one, for which there is no code, as NaN.  The update itself uses m and v before they are rounded.
 // What is stored in a code is rounded to fp32 as the formulas are written, products, root and quotient each to the nearest: a
 // value one step of fp32 off would now and then take the neighbouring code, an eighth away, and with it the steps behind.
 //
@@ -172,7 +172,7 @@ __device__ __forceinline__ void update(const Lane<P, G, MASTER, BITS>& l, const 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       m[j] = quotient(m[j], mu, im);
-      r[j] = r[j] > 0.f ? fmaxf(quotient(r[j], ru, ir), kLeast) : r[j];
+      r[j] = r[j] > 0.f && r[j] < INFINITY ? fmaxf(quotient(r[j], ru, ir), kLeast) : r[j] > 0.f ? NAN : r[j];
     }
     write_codes<FULL>((uint8_t*)e.m + at, c, n, encode(m));
     write_codes<FULL>((uint8_t*)e.v + at, c, n, encode(r));

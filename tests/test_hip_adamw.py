@@ -207,6 +207,35 @@ def test_gradients_that_are_not_finite(bits):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("huge", [1e20, -3e38, float("inf"), float("nan")])
+def test_squares_that_overflow(huge, bits):
+    """An infinite v stays that in 32 bits, and is NaN in 8: never a finite code, beside which the next step would be unbounded."""
+    s, n, at = _state([600], torch.float32, torch.float32, False, bits, seed=6), 600, 300
+    s["g"][0][at] = huge
+    w = s["p"][0].clone()
+    _go(s, wd=0.0)
+    rest = torch.arange(n, device=DEV) != at
+    m, v = s["m"][0].float()[at], s["v"][0].float()[at]
+    finite = abs(huge) < 1e39
+    if bits == 32:
+        assert torch.isinf(v) if huge == huge else torch.isnan(v)
+    else:
+        assert torch.isnan(v) and torch.isfinite(s["vs"][0]).all() and (finite or torch.isnan(m))
+    assert s["p"][0][at] == w[at] if finite else torch.isnan(s["p"][0][at])
+    assert ((s["p"][0] - w)[rest].abs() < 1.01e-3).all()
+    s["g"][0].zero_()
+    for _ in range(3):
+        before = s["p"][0].clone()
+        _go(s, wd=0.0)
+        if finite and bits == 32:
+            assert s["p"][0][at] == w[at]
+        else:
+            assert torch.isnan(s["p"][0][at])
+        assert ((s["p"][0] - before)[rest].abs() < 1.5e-3).all()      # (m / sqrt(v) of one gradient falls from 1 by less than its sum)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
 def test_zero_gradients_and_decay(bits):
     """Nothing but the decay moves; states stay zero; eps = 0 would divide zero by zero."""
     s = _state([5000], torch.float32, torch.float32, False, bits)
