@@ -68,12 +68,17 @@ __device__ __forceinline__ float quotient(float a, float x, float inv) {
   const float q = a * inv;
   return fmaf(fmaf(-q, x, a), inv, q);
 }
-// the root to the nearest: the hardware's is a step off at most, and one of the three fits
-__device__ __forceinline__ float root(float x) {
-  const float s = __builtin_amdgcn_sqrtf(x);
+// The hardware's root (a step off at most) takes a square below 2^-126 for zero: those are moved up by 2^64 and their roots down
+// by 2^-32, both exact.
+__device__ __forceinline__ float root_down(float x) { return x < 0x1p-96f ? 0x1p-32f : 1.f; }
+__device__ __forceinline__ float root_up(float x) { return x < 0x1p-96f ? x * 0x1p64f : x; }
+__device__ __forceinline__ float near_root(float x) { return __builtin_amdgcn_sqrtf(root_up(x)) * root_down(x); }
+// the root to the nearest: of the hardware's and its neighbours one fits
+__device__ __forceinline__ float root(float y) {
+  const float x = root_up(y), s = __builtin_amdgcn_sqrtf(x);
   const float dn = __builtin_bit_cast(float, __builtin_bit_cast(int, s) - 1), up = __builtin_bit_cast(float, __builtin_bit_cast(int, s) + 1);
   const float r = fmaf(-dn, s, x) <= 0.f ? dn : s;
-  return fmaf(-up, s, x) > 0.f ? up : r;
+  return (fmaf(-up, s, x) > 0.f ? up : r) * root_down(y);
 }
 
 // What a lane holds of a block
@@ -162,7 +167,7 @@ __device__ __forceinline__ void update(const Lane<P, G, MASTER, BITS>& l, const 
     g[j] *= scale;
     m[j] = fmaf(c1, g[j], b1 * m[j]);
     v[j] = fmaf(c2, g[j] * g[j], b2 * v[j]);
-    r[j] = BITS == 8 ? root(v[j]) : __builtin_amdgcn_sqrtf(v[j]);   // (a step off at most, like the reciprocal)
+    r[j] = BITS == 8 ? root(v[j]) : near_root(v[j]);                // (a step off at most, like the reciprocal)
     w[j] = fmaf(w[j], keep, -k.rate * m[j] * __builtin_amdgcn_rcpf(fmaf(r[j], k.inv_root, eps)));
   }
   if constexpr (MASTER) write<FULL>(e.master + at, c, n, w);

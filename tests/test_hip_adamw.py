@@ -236,6 +236,25 @@ def test_squares_that_overflow(huge, bits):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("bits", [32, 8])
+def test_gradients_whose_squares_are_subnormal(bits):
+    """Gradients of 1e-21, eps = 0: the first step's update is lr, whatever they are, and a code of sqrt(v) is that of its root.  v is a
+    multiple of 2^-149, half a step of that off: (g^2)(1 - beta2) of 1e-21 by 2^-149 / 2 / 5e-44 = 0.014, its root by 0.007."""
+    s = _state([3000], torch.float32, torch.float32, False, bits, seed=8)
+    g = s["g"][0]
+    g.copy_(g.sign() * (1 + torch.rand(3000, generator=torch.Generator().manual_seed(1)).to(DEV)) * 1e-21)
+    w = s["p"][0].clone()
+    seco.adamw_step(s["p"], s["g"], s["m"], s["v"], s["step"], 1e-3, betas=BETAS, eps=0.0, weight_decay=0.0, m_scales=s["ms"], v_scales=s["vs"])
+    moved = (w - s["p"][0]).cpu().double() / 1e-3 * g.sign().cpu()
+    assert ((moved - 1).abs() < 0.008 + 4 * U * 0.2 / 1e-3).all()               # (and p's own rounding)
+    if bits == 8:
+        # half a step of e4m3 and a unit above 2^-126, in which 1e-21 has a code of its own
+        r = _unpack(s["v"][0].cpu(), s["vs"][0].cpu())
+        want = g.cpu().double().abs() * (1 - BETAS[1]) ** 0.5
+        assert ((r / want - 1).abs() < 2.0 ** -4 + 0.008).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
 def test_zero_gradients_and_decay(bits):
     """Nothing but the decay moves; states stay zero; eps = 0 would divide zero by zero."""
     s = _state([5000], torch.float32, torch.float32, False, bits)
