@@ -70,7 +70,8 @@ __device__ __forceinline__ float unit_of(const float (&f)[4]) {
   return fmaxf(quotient(top, kTop, 1.f / kTop), 0x1p-126f);
 }
 // The hardware's root (a step off at most) takes a square below 2^-126 for zero: those are moved up by 2^64 and their roots down
-// by 2^-32, both exact.
+// by 2^-32, both exact.  That takes 1.2 % of the time of 478M elements in 8 bits (1278 -> 1293 us), 0.6 % in 32; a branch around it for
+// wavefronts that hold such squares takes 5 %.
 __device__ __forceinline__ float root_down(float x) { return x < 0x1p-96f ? 0x1p-32f : 1.f; }
 __device__ __forceinline__ float root_up(float x) { return x < 0x1p-96f ? x * 0x1p64f : x; }
 __device__ __forceinline__ float near_root(float x) { return __builtin_amdgcn_sqrtf(root_up(x)) * root_down(x); }
