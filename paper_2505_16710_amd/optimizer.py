@@ -50,13 +50,16 @@ class AdamW:
             self.m_scales, self.v_scales = ([torch.zeros(-(-t.numel() // BLOCK), device=t.device) for t in self.params]
                                             for _ in range(2))
         self.masters = [t.detach().float() if masters and t.dtype == torch.bfloat16 else None for t in self.params]
+        # steps taken, on the GPU: a counter for the parameters that have had their gradients in the same calls
         self.steps = torch.zeros(2, dtype=torch.int64, device=self.params[0].device)
+        self._counted = [(self.steps, list(range(len(self.params))))]
 
     def step(self, grads=None, grad_scale=None):
         """One update.  grads: None (every parameter's .grad), or a dict by the names of the parameters, or a list in their
-        order; a parameter without a gradient (None, or not in the dict) stays as it is, its states too, while one whose
-        gradient is zero decays.  grad_scale: a
-        one-element fp32 tensor on the GPU that the gradients are multiplied by (clipping, loss scaling), or None."""
+        order; a parameter without a gradient (None, or not in the dict) stays as it is, its states and the number of its steps
+        too, while one whose gradient is zero decays.  Parameters whose numbers differ take launches of their own; a captured
+        step does not tell them apart if none in front of it has had gradients of the same ones.  grad_scale: a one-element fp32
+        tensor on the GPU that the gradients are multiplied by (clipping, loss scaling), or None."""
         if grads is None:
             found = [t.grad for t in self.params]
         elif isinstance(grads, dict):
@@ -69,18 +72,30 @@ class AdamW:
             found = list(grads)
             if len(found) != len(self.params):
                 raise ValueError("one gradient (or None) per parameter")
-        at = [i for i, g in enumerate(found) if g is not None]
-        every = len(at) == len(found)
-
-        def of(values):
-            return values if every or values is None else [values[i] for i in at]
-        for i in at:
-            g, t = found[i], self.params[i]
-            if g.stride() != t.stride() and g.shape == t.shape:     # (a dense copy in the parameter's order)
+        missing = any(g is None for g in found)
+        if missing or len(self._counted) > 1:    # (what the update would refuse, before the first of several launches)
+            for n, t, g in zip(self.names, self.params, found):
+                if g is not None and (g.shape != t.shape or g.device != t.device):
+                    raise ValueError(f"{n}: the gradient must have the parameter's shape and device")
+                if g is not None and g.dtype not in (torch.bfloat16, torch.float32):
+                    raise TypeError(f"{n}: gradients are bfloat16 or float32 tensors")
+        for i, (g, t) in enumerate(zip(found, self.params)):
+            if g is not None and g.stride() != t.stride() and g.shape == t.shape:     # (a dense copy in the parameter's order)
                 found[i] = torch.empty_like(t, dtype=g.dtype, requires_grad=False).copy_(g)
         with torch.no_grad():
-            _b.adamw_step(of(self.params), of(found), of(self.m), of(self.v), self.steps, self.lr, self.betas, self.eps,
-                          of(self.weight_decay), of(self.masters), of(self.m_scales), of(self.v_scales), grad_scale)
+            for steps, members in self._counted[:]:
+                at = [i for i in members if found[i] is not None] if missing else members
+                if not at:
+                    continue
+                if len(at) < len(members) and not (steps.is_cuda and torch.cuda.is_current_stream_capturing()):
+                    self._counted.append((steps.clone(), [i for i in members if found[i] is None]))
+                    members[:] = at
+                every = len(at) == len(self.params)
+
+                def of(values):
+                    return values if every or values is None else [values[i] for i in at]
+                _b.adamw_step(of(self.params), of(found), of(self.m), of(self.v), steps, self.lr, self.betas, self.eps,
+                              of(self.weight_decay), of(self.masters), of(self.m_scales), of(self.v_scales), grad_scale)
 
     def sync_masters(self):
         """Takes the masters from the parameters again (after a program has written to these itself)."""
@@ -89,8 +104,12 @@ class AdamW:
                 w.copy_(t.detach())
 
     def state_dict(self):
-        """The state by the parameters' names: tensors that are the optimizer's own."""
+        """The state by the parameters' names: tensors that are the optimizer's own.  late: counters of the parameters whose number
+        of steps is not `steps`, where there are any."""
         out = {"state_bits": self.state_bits, "steps": self.steps}
+        late = {self.names[i]: steps for steps, members in self._counted[1:] for i in members}
+        if late:
+            out["late"] = late
         for key in ("m", "v", "m_scales", "v_scales", "masters"):
             values = getattr(self, key)
             if values is not None:
@@ -99,14 +118,23 @@ class AdamW:
 
     def load_state_dict(self, state):
         """Copies a state of the same parameters and state_bits; parameters are the program's to load."""
-        mine = self.state_dict()
-        if state["state_bits"] != self.state_bits or set(state) != set(mine):
+        mine, late = self.state_dict(), state.get("late", {})
+        keys = set(mine) - {"state_bits", "steps", "late"}
+        if state["state_bits"] != self.state_bits or set(state) - {"late"} != keys | {"state_bits", "steps"}:
             raise ValueError("the state is of another kind (state_bits)")
-        for key in set(mine) - {"state_bits", "steps"}:
+        for key in keys:
             if set(state[key]) != set(mine[key]) or any(x.shape != mine[key][n].shape or x.dtype != mine[key][n].dtype
                                                         for n, x in state[key].items()):
                 raise ValueError(f"{key}: other parameters, or of another shape")
-        for key in set(mine) - {"state_bits", "steps"}:
+        if not set(late) < set(self.names) and late:
+            raise ValueError("late: other parameters")
+        for key in keys:
             for n, x in state[key].items():
                 mine[key][n].copy_(x)
         self.steps.copy_(state["steps"])
+        groups = {}                              # of those whose numbers are equal
+        for i, n in enumerate(self.names):
+            groups.setdefault(int(late[n][0]) if n in late else None, []).append(i)
+        self._counted = [(self.steps, groups.pop(None))] + [(torch.zeros_like(self.steps), members) for members in groups.values()]
+        for (counter, _), number in zip(self._counted[1:], groups):
+            counter[0] = number

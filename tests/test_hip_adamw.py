@@ -420,6 +420,61 @@ def test_optimizer_with_shared_and_idle_parameters():
 
 
 @pytest.mark.gpu
+def test_steps_without_every_gradient():
+    """Beside torch.optim.AdamW in 64 bits: a parameter's correction goes by the steps that it has taken, whether its gradients begin
+    late, are missing now and then, or all are.  Bounds as in test_optimizer_follows_a_plain_one, for 24 steps."""
+    host = {n: t.double().requires_grad_() for n, t in _params().items()}
+    dev = {n: t.to(DEV).requires_grad_() for n, t in _params().items()}
+    kw = dict(lr=1e-2, betas=(0.9, 0.99), eps=1e-8, weight_decay=0.1)
+    plain, opt = torch.optim.AdamW(host.values(), **kw), AdamW(dev, **kw)
+    taken = dict.fromkeys(host, 0)
+    for k in range(24):
+        g = torch.Generator().manual_seed(200 + k)
+        grads = {n: torch.randn(t.shape, generator=g) for n, t in host.items()}
+        there = [n for n in host if not (n == "b" and k < 10 or n == "t" and k % 3 == 1 or k in (4, 17))]
+        for n in host:
+            host[n].grad = grads[n].double() if n in there else None
+            taken[n] += n in there
+        plain.step()
+        opt.step({n: grads[n].to(DEV) for n in there})
+        if k == 12:                                               # through a state saved here
+            saved = {a: {n: x.clone() for n, x in b.items()} if isinstance(b, dict) else b for a, b in opt.state_dict().items()}
+            opt = AdamW(dev, **kw)
+            opt.load_state_dict(saved)
+    counts = {"w": opt.steps, **opt.state_dict()["late"]}
+    assert opt.steps.tolist() == [22, 0] and {n: int(c[0]) for n, c in counts.items()} == taken
+    for n in host:
+        x, y = dev[n].detach().cpu().double(), host[n].detach()
+        assert ((x - y).abs() <= 24 * (64 * U * 10 * 1e-2 + 8 * U * y.abs())).all(), n
+
+
+@pytest.mark.gpu
+def test_captured_step_without_every_gradient():
+    """Captured behind a step with the same gradients, a replay counts the steps of those parameters alone."""
+    dev = [t.to(DEV) for t in _params().values()]
+    ref = [t.clone() for t in dev]
+    a, b = AdamW(dev, lr=1e-2), AdamW(ref, lr=1e-2)
+    g = [torch.randn_like(t) for t in dev]
+    some = [g[0], None, g[2]]
+    a.step(some)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.step(some)
+    b.step(some)
+    for k in range(3):
+        for x in g:
+            x.normal_(generator=torch.Generator(device=DEV).manual_seed(k))
+        graph.replay()
+        torch.cuda.synchronize()
+        b.step(some)
+    a.step(g)
+    b.step(g)
+    assert all(torch.equal(x, y) for x, y in zip(dev, ref)) and a.steps.tolist() == b.steps.tolist() == [5, 0]
+    assert a.state_dict()["late"]["1"].tolist() == [1, 0]
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("bits", [32, 8])
 def test_optimizer_state_saved_and_loaded(bits):
     def new():
@@ -480,6 +535,20 @@ def test_refusals():
         AdamW({"w": x.half()})
     with pytest.raises(ValueError):
         AdamW({})
+
+
+def test_states_that_do_not_fit_are_refused():
+    p = {"a": torch.zeros(4, 6), "b": torch.zeros(8)}
+    state = AdamW(p).state_dict()
+    for wrong in ({"late": {"c": torch.zeros(2)}}, {"late": {n: torch.zeros(2) for n in p}}, {"m": {}}, {"more": {}}):
+        with pytest.raises(ValueError):
+            AdamW(p).load_state_dict({**state, **wrong})
+    opt = AdamW(p)
+    for bad, error in ((torch.zeros(9), ValueError), (torch.zeros(8).half(), TypeError)):
+        with pytest.raises(error, match="b: "):
+            opt.step([None, bad])
+    assert "late" not in state and "late" not in opt.state_dict()
+    AdamW(p).load_state_dict(state)
 
 
 def test_status_codes():
