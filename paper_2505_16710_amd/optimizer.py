@@ -17,6 +17,11 @@ from . import binding as _b
 BLOCK = 256                                      # elements that share a unit of the 8-bit states
 
 
+def _order(t):
+    """Where the elements of a dense tensor lie, beside their shape."""
+    return [(n, s) for n, s in zip(t.shape, t.stride()) if n > 1] if t.numel() else []
+
+
 class AdamW:
     """params: a dict name -> tensor, or an iterable of tensors (bf16 or fp32, dense in memory, on one GPU); a tensor that is
     there under several names is updated once.  lr: a float, or a one-element fp32 tensor on the GPU, which a captured step
@@ -126,6 +131,8 @@ class AdamW:
             if set(state[key]) != set(mine[key]) or any(x.shape != mine[key][n].shape or x.dtype != mine[key][n].dtype
                                                         for n, x in state[key].items()):
                 raise ValueError(f"{key}: other parameters, or of another shape")
+            if self.state_bits == 8 and key in ("m", "v") and any(_order(x) != _order(mine[key][n]) for n, x in state[key].items()):
+                raise ValueError(f"{key}: saved from parameters whose dimensions lie in another order, and with it their blocks")
         if not set(late) < set(self.names) and late:
             raise ValueError("late: other parameters")
         for key in keys:

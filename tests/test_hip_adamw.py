@@ -551,6 +551,23 @@ def test_states_that_do_not_fit_are_refused():
     AdamW(p).load_state_dict(state)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_states_of_another_order_of_dimensions(bits):
+    """Units of 8-bit states belong to blocks in the order of memory: codes of the same shape in another order do not fit them."""
+    rows, columns, one = torch.zeros(40, 20), torch.zeros(20, 40).t(), torch.zeros(40, 1, 20).transpose(0, 1)
+    state = AdamW({"w": columns}, state_bits=bits).state_dict()
+    state["m"]["w"].copy_(torch.arange(800.0).view(40, 20))
+    opt = AdamW({"w": rows}, state_bits=bits)
+    if bits == 8:
+        with pytest.raises(ValueError, match="order"):
+            opt.load_state_dict(state)
+        opt.load_state_dict(AdamW({"w": rows.clone()}, state_bits=8).state_dict())
+    else:
+        opt.load_state_dict(state)
+        assert torch.equal(opt.m[0], torch.arange(800.0).view(40, 20))
+    AdamW({"w": one}, state_bits=bits).load_state_dict(AdamW({"w": torch.zeros(1, 40, 20)}, state_bits=bits).state_dict())
+
+
 def test_status_codes():
     lib = seco.load_library()
 
