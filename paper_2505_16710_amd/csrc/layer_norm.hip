@@ -921,7 +921,7 @@ template <typename T> int norm_bwd_few(NormArgs a, bool rows, bool sums, hipStre
 // Up to 1280 rows; beyond, the walk down the rows is the longest way.  us, one launch / parts and their sums, tensors out of memory:
 // bf16 1100 x 100 6.2 / 8.3, 1100 x 1024 9.2 / 9.6, 1100 x 4096 14.5 / 21.1, 1000 x 16384 47 / 60, fp32 300 x 15520 24 / 34, 1000 x 8192
 // 34.6 / 39.3; 1500 rows between 6.6 / 7.8 (100 elements) and 11.4 / 10.6 (1000), 2048 x 1024 14.3 / 10.2, 3000 x 512 18.2 / 7.8.
-bool norm_few(int64_t rows, int64_t d) { return rows >= 1 && rows <= 1280 && d <= 16384; }         // (16384: backward_shape's longest)
+bool norm_few(int64_t rows, int64_t d) { return rows >= 1 && rows <= kNormFewRows && d <= kNormFewLength; }
 int launch_norm_bwd_few(const NormArgs& a, bool rows, bool sums, hipStream_t s) {
   return a.dtype == SECO_BF16 ? norm_bwd_few<__bf16>(a, rows, sums, s) : norm_bwd_few<float>(a, rows, sums, s);
 }

@@ -33,6 +33,10 @@ struct NormArgs {
 int norm_blocks(int64_t rows, int64_t d, int dtype);                       // workgroups of a backward call
 int launch_norm_fwd(const NormArgs& a, hipStream_t s);
 int launch_norm_bwd(const NormArgs& a, hipStream_t s);
+// Rows of a backward call in one launch, and their length (backward_shape's longest).  A test of refusals hands calls of 2000 rows
+// without a workspace to the library, with addresses that no kernel may see.
+constexpr int64_t kNormFewRows = 1280, kNormFewLength = 16384;
+static_assert(kNormFewRows < 2000, "calls of 2000 rows have to bring a workspace");
 // Whether a backward call has so few rows that its sums need no parts, but come from a.x and a.dy a second time; and that call:
 // d_x (rows), the sums, or both in one launch where d_x overwrites neither
 bool norm_few(int64_t rows, int64_t d);
