@@ -128,6 +128,45 @@ def test_backward_of_long_rows(t, d, rows, d_in):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t,d,rows,d_in", [("bf16", 2056, 1301, "none"), ("bf16", 4099, 1301, "in place"), ("bf16", 8192, 1290, "apart"),
+                                           ("bf16", 12001, 1301, "in place"), ("bf16", 12001, 1400, "apart"), ("bf16", 16384, 1281, "none"),
+                                           ("f32", 2051, 1301, "in place"), ("f32", 4097, 1301, "in place"), ("f32", 8192, 1283, "apart")])
+def test_backward_of_more_wide_rows_than_one_launch_takes(t, d, rows, d_in):
+    """A workgroup to several rows in turn, at every number of words to a lane; what is left over does not come out even."""
+    _check_backward(t, d, rows, d_in)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("t,d,rows", [("bf16", 1024, 1500), ("bf16", 2056, 1500), ("bf16", 4099, 700), ("bf16", 4099, 1301), ("bf16", 8192, 1290),
+                                      ("bf16", 12001, 1301), ("bf16", 16400, 600), ("f32", 2051, 1301), ("f32", 8192, 1283), ("f32", 8195, 1400)])
+def test_shares_of_a_training_step_are_added_to(t, d, rows):
+    """As the step calls it: shares of the sums on top of what is there, chunk after chunk, d_x in the place of d_in."""
+    import ctypes as C
+    dtype, U1 = TYPES[t], 64 * U
+    gain = _rows(d + 7, 1, d, dtype)[0].contiguous()
+    parts = torch.randn(2, 256, d, generator=torch.Generator().manual_seed(d)).to(DEV)
+    want, size = parts.double().sum(1).cpu(), parts.double().abs().sum(1).cpu()
+    lib = seco.load_library()
+    gd = gain.to(DEV)
+    for k in range(2):
+        x, dy, extra = (_rows(10 * k + i, rows, d, dtype) for i in range(3))
+        mean, rstd, _ = _forward64(x, None, None, 1e-5)
+        mean, rstd = mean.float(), rstd.float()
+        at = [a.to(DEV) for a in (x, mean, rstd, dy, extra)]
+        p = [C.c_void_p(a.data_ptr()) for a in at]
+        apart = seco.layer_norm_bwd(at[0], gd, at[1], at[2], at[3], d_in=at[4])[0]
+        rc = lib.dec_layer_norm_bwd(C.c_int(1 if t == "bf16" else 0), p[0], C.c_void_p(gd.data_ptr()), p[1], p[2], p[3], p[4], p[4],
+                                    C.c_void_p(parts.data_ptr()), C.c_int64(rows), C.c_int64(d),
+                                    C.c_void_p(torch.cuda.current_stream().cuda_stream))
+        assert rc == 0 and torch.equal(at[4], apart)
+        n = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+        n_size = n.abs() + 2 * (x.double().abs() + mean.double().abs()[:, None]) * rstd.double()[:, None] / 64
+        want += torch.stack([(dy.double() * n).sum(0), dy.double().sum(0)])
+        size += torch.stack([(dy.double().abs() * n_size).sum(0), dy.double().abs().sum(0)])
+        assert ((parts.double().sum(1).cpu() - want).abs() <= U1 * size).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("t", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,d", [(1, 3), (2, 1024), (129, 45), (513, 260), (1024, 1027), (1280, 1027), (1281, 1027), (1900, 333), (1400, 4100), (300, 16384), (40, 16390), (100, 12001), (1040, 16391)])
 def test_where_the_results_lie_changes_nothing(t, rows, d):
@@ -163,6 +202,12 @@ def test_gradient_added_in_place(t, rows, d):
     place = extra.clone()
     got = seco.layer_norm_bwd(x, None, mean, rstd, dy, d_in=place, d_x=place)
     assert got[0] is place and all(torch.equal(a, b) for a, b in zip(got, apart))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("t,rows,d", [("bf16", 1400, 12001), ("bf16", 1300, 8203), ("bf16", 1301, 16381), ("f32", 1300, 8190)])
+def test_gradient_added_in_place_of_more_rows(t, rows, d):
+    test_gradient_added_in_place(t, rows, d)
 
 
 @pytest.mark.gpu
