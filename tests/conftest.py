@@ -18,6 +18,13 @@ def _gpu_available():
         return False
 
 
+def pytest_runtest_setup(item):
+    """Tests that draw without a generator of their own draw the same numbers every time: one of the oracle's pins compares sums to
+    1e-14 of themselves, which one draw in 300 lets cancel."""
+    import torch
+    torch.manual_seed(0)
+
+
 def pytest_collection_modifyitems(config, items):
     if _gpu_available():
         return
