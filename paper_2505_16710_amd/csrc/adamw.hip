@@ -8,9 +8,8 @@
 // decay by b2 = 0.999 a step keeps its codes and follows in its unit, while a single code could not move by so little.  r instead
 // of v: its three bits and 18 powers of two of range then hold v over 36.  An r that is not zero is never stored as
 // zero (its m / eps would be unbounded), but as at least the smallest code; an infinite one, for which there is no code, as NaN.  The update itself uses m and v before they are rounded.
-// What is stored is rounded to fp32 as the formulas are written (b m a product, to which (1 - b) g is added in one fused operation),
-// products, root, unit and quotients each to the nearest: a value one step of fp32 off would now and then take the neighbouring code,
-// an eighth away, and with it the steps behind.
+// What is stored in a code is rounded to fp32 as the formulas are written, products, root and quotient each to the nearest: a
+// value one step of fp32 off would now and then take the neighbouring code, an eighth away, and with it the steps behind.
 //
 // Bound by memory: 28 bytes per element with fp32 masters and states, 16.06 with states of 8 bits.  A wavefront takes a block at
 // a time, 4 elements to a lane, so that a block's largest magnitudes are a reduction over its lanes.
@@ -49,15 +48,6 @@ __device__ __forceinline__ unsigned encode(const float (&f)[4]) {
   const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
   return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], lo, true);
 }
-// 1 / x and a / x, given 1 / x, to the nearest: one correction of what is a step off at most
-__device__ __forceinline__ float reciprocal(float x) {
-  const float r = __builtin_amdgcn_rcpf(x);
-  return fmaf(fmaf(-x, r, 1.f), r, r);
-}
-__device__ __forceinline__ float quotient(float a, float x, float inv) {
-  const float q = a * inv;
-  return fmaf(fmaf(-q, x, a), inv, q);
-}
 // the largest finite magnitude of a block / 448, in every lane
 __device__ __forceinline__ float unit_of(const float (&f)[4]) {
   float top = wave_max(fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3]))));   // (without the NaN)
@@ -67,7 +57,16 @@ __device__ __forceinline__ float unit_of(const float (&f)[4]) {
     for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(f[j]) < INFINITY ? fabsf(f[j]) : 0.f);
     top = wave_max(top);
   }
-  return fmaxf(quotient(top, kTop, 1.f / kTop), 0x1p-126f);
+  return fmaxf(top * (1.f / kTop), 0x1p-126f);
+}
+// 1 / x and a / x, given 1 / x, to the nearest: one correction of what is a step off at most
+__device__ __forceinline__ float reciprocal(float x) {
+  const float r = __builtin_amdgcn_rcpf(x);
+  return fmaf(fmaf(-x, r, 1.f), r, r);
+}
+__device__ __forceinline__ float quotient(float a, float x, float inv) {
+  const float q = a * inv;
+  return fmaf(fmaf(-q, x, a), inv, q);
 }
 // The hardware's root (a step off at most) takes a square below 2^-126 for zero: those are moved up by 2^64 and their roots down
 // by 2^-32, both exact.  That takes 1.2 % of the time of 478M elements in 8 bits (1278 -> 1293 us), 0.6 % in 32; a branch around it for
