@@ -382,7 +382,7 @@ size_t layer_norm_workspace_bytes(const layer_norm_desc* desc);
  *   param         in/out; master (fp32, bf16 parameters only, or NULL): what is updated instead, the parameter is its rounding
  *   m, v          state_bits 32: fp32 [n].  state_bits 8: e4m3 codes [n] of m and of sqrt(v), in units of m_scale, v_scale:
  *                 one fp32 per 256 consecutive elements of the tensor (the last block may be short), the block's largest finite
- *                 magnitude / 448 (at least 2^-126).  A sqrt(v) > 0 is stored as at least the smallest code, 2^-9.  The update
+ *                 magnitude times the fp32 value of 1 / 448 (at least 2^-126).  A sqrt(v) > 0 is stored as at least the smallest code, 2^-9.  The update
  *                 uses m and v before they are rounded.  All zeros (codes and scales) is the state before the first step.
  *   step          device, two int64: [0] steps taken so far, read and incremented by the call (so that a captured graph
  *                 counts on when it is replayed); [1] the call's own, 0 before and after every call

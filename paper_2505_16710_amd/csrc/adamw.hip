@@ -8,8 +8,9 @@
 // decay by b2 = 0.999 a step keeps its codes and follows in its unit, while a single code could not move by so little.  r instead
 // of v: its three bits and 18 powers of two of range then hold v over 36.  An r that is not zero is never stored as
 // zero (its m / eps would be unbounded), but as at least the smallest code; an infinite one, for which there is no code, as NaN.  The update itself uses m and v before they are rounded.
-// What is stored in a code is rounded to fp32 as the formulas are written, products, root and quotient each to the nearest: a
-// value one step of fp32 off would now and then take the neighbouring code, an eighth away, and with it the steps behind.
+// What is stored is rounded to fp32 operation by operation: (1 - b) g is added to the product b m in one fused operation, the unit is
+// the largest magnitude times the rounded 1 / 448, root and quotient are to the nearest.  A value one step of fp32 off would now and
+// then take the neighbouring code, an eighth away, and with it the steps behind.
 //
 // Bound by memory: 28 bytes per element with fp32 masters and states, 16.06 with states of 8 bits.  A wavefront takes a block at
 // a time, 4 elements to a lane, so that a block's largest magnitudes are a reduction over its lanes.

@@ -254,6 +254,26 @@ def test_gradients_whose_squares_are_subnormal(bits):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("low,high", [(-8, 4), (-22, -16), (14, 18)])
+def test_units_and_codes_are_the_formulas(low, high):
+    """With betas of zero m is g and sqrt(v) is sqrt(g^2): units and codes are, bit by bit, those of fp32 operations to the nearest."""
+    n = 256 * 400
+    gen = torch.Generator().manual_seed(high)
+    g = (torch.randn(n // 256, 256, generator=gen) * 10.0 ** (low + (high - low) * torch.rand(n // 256, 1, generator=gen))).reshape(-1)
+    s = _state([n], torch.float32, torch.float32, False, 8)
+    s["g"][0].copy_(g)
+    seco.adamw_step(s["p"], s["g"], s["m"], s["v"], s["step"], 1e-3, betas=(0.0, 0.0), m_scales=s["ms"], v_scales=s["vs"])
+    for x, codes, scale in ((g, s["m"][0], s["ms"][0]), ((g * g).sqrt(), s["v"][0], s["vs"][0])):
+        x = x.view(-1, 256)
+        unit = (x.abs().amax(1) * torch.tensor(1 / 448)).clamp_min(2.0 ** -126)
+        assert torch.equal(scale.cpu(), unit)
+        want = (x / unit[:, None]).clamp(-448, 448).to(torch.float8_e4m3fn).float()
+        if scale is s["vs"][0]:
+            want = torch.where((x > 0) & (want < 2.0 ** -9), 2.0 ** -9, want)
+        assert torch.equal(codes.float().cpu().view(-1, 256), want)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("bits", [32, 8])
 def test_zero_gradients_and_decay(bits):
     """Nothing but the decay moves; states stay zero; eps = 0 would divide zero by zero."""
