@@ -189,12 +189,12 @@ def hand_over(params, grads):
             total[id(t)] = total[id(t)] + g if id(t) in total else g
     roots = {}                                  # id -> parameter: what takes its gradient through autograd
     for t in params.values():
-        if id(t) in total:
-            plain = t.is_leaf and not has_grad_hooks(t)
-            if t.is_leaf:
-                t.grad = total[id(t)] if plain else None
-            if not plain:
-                roots[id(t)] = t
+        g = total.get(id(t))
+        plain = g is None or (t.is_leaf and not has_grad_hooks(t))
+        if t.is_leaf:
+            t.grad = g if plain else None
+        if not plain:
+            roots[id(t)] = t
     if roots:                                   # (in one pass, behind all assignments: no order of the names loses a share)
         torch.autograd.backward(list(roots.values()), [total[i] for i in roots])
     out = {}

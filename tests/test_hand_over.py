@@ -56,6 +56,8 @@ def test_a_second_step_takes_the_place_of_the_first():
         out = hand_over({"a": a, "b": b, "c": c}, {n: torch.full((3,), k) for n in "abc"})
         assert torch.equal(a.grad, torch.full((3,), 10 * k)) and torch.equal(out["a"], a.grad)
         assert torch.equal(b.grad, torch.full((3,), k)) and torch.equal(c.grad, torch.full((3,), k))
+    out = hand_over({"a": a, "b": b, "c": c}, {"a": None, "b": None, "c": None})       # (no chunk reached them)
+    assert a.grad is None and b.grad is None and c.grad is None and not any(t.any() for t in out.values())
 
 
 @pytest.mark.parametrize("hooked", [False, True])
