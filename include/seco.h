@@ -345,10 +345,10 @@ int rope_readout_axes(const seco_desc* desc, const rope_axes* axes, const void* 
  *              d_gain = sum over rows of d_y * n,  d_bias = sum over rows of d_y   (fixed order: reproducible)
  * gain, bias   [d] of gain_dtype, or NULL (ones, zeros)
  * mean, rstd   fp32 [rows], one behind the other
- * residual and x_out go together, both or neither; x_out may be x or residual, y may be x when there is no residual (same
- * stride).  Else results share no memory with what is read, nor with each other.  d_in may be NULL (nothing is added); d_x may be
- * x, d_y or d_in (same stride).  In the backward, x is the row that
- * was normalised: x_out where there was a residual.  d_gain, d_bias: overwritten; NULL: not wanted.
+ * residual and x_out go together, both or neither.  y and x_out may each be x or residual (same stride); d_x may be x, d_y or
+ * d_in (same stride).  Else results share no memory with what is read, nor with each other.  d_in may be NULL (nothing is
+ * added).  In the backward, x is the row that was normalised: x_out where there was a residual.  d_gain, d_bias: overwritten;
+ * NULL: not wanted.
  * rows = 0 is allowed (d_gain and d_bias are then zeros).  Row strides of inputs may be 0 (one row for all).
  * ws of the backward: layer_norm_workspace_bytes(desc) bytes, 16-byte aligned; not needed (NULL) where these are 0, or when
  * neither d_gain nor d_bias is wanted.

@@ -278,8 +278,8 @@ def rope_readout_axes(d_q, gk, gv, row_begin, positions, axes, scaler=1.0, dq_ou
 def layer_norm_fwd(x, gain=None, bias=None, eps=1e-5, residual=None, y=None, x_out=None, stream=None):
     """Layer norm of the rows of x [..., d] (bf16 or fp32; rows contiguous, at one distance from each other).
     Returns (y, mean, rstd), mean and rstd fp32 [...]; with a residual (shape and dtype of x) that is added first, (y, mean,
-    rstd, x_out) with x_out = x + residual, rounded.  gain, bias: [d] of x's dtype or fp32, or None.  y may be x without a
-    residual, x_out may be x or residual; results that overlap in another way are refused, here and in the calls around."""
+    rstd, x_out) with x_out = x + residual, rounded.  gain, bias: [d] of x's dtype or fp32, or None.  y and x_out may
+    each be x or residual; results that overlap in another way are refused, here and in the calls around."""
     return (_ext or _load_ext()).norm_fwd(x, gain, bias, eps, residual, y, x_out, stream)
 
 

@@ -128,6 +128,24 @@ def test_backward_of_long_rows(t, d, rows, d_in):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t,d", [("bf16", 5), ("bf16", 96), ("bf16", 250), ("bf16", 1027), ("bf16", 2056), ("bf16", 4099), ("bf16", 12001), ("bf16", 20001),
+                                 ("f32", 1027), ("f32", 8002), ("f32", 17001)])
+@pytest.mark.parametrize("rows", [3, 2100])
+def test_forward_results_in_the_place_of_either_input(t, d, rows):
+    """y in the place of x or of the residual, x_out in that of the other, or apart: the same bits."""
+    dtype = TYPES[t]
+    x, r = (_on_gpu(_rows(64 + i, min(rows, (1 << 23) // d), d, dtype)) for i in range(2))
+    want = seco.layer_norm_fwd(x, residual=r)
+    for y_at, out_at in (("x", None), ("r", None), ("x", "r"), ("r", "x")):
+        a = {"x": x.clone(), "r": r.clone(), None: None}
+        got = seco.layer_norm_fwd(a["x"], residual=a["r"], y=a[y_at], x_out=a[out_at])
+        assert got[0] is a[y_at] and all(torch.equal(p, q) for p, q in zip(got, want))
+    place = x.clone()
+    alone = seco.layer_norm_fwd(x)
+    assert all(torch.equal(p, q) for p, q in zip(seco.layer_norm_fwd(place, y=place), alone))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("t,d,rows,d_in", [("bf16", 2056, 1301, "none"), ("bf16", 4099, 1301, "in place"), ("bf16", 8192, 1290, "apart"),
                                            ("bf16", 12001, 1301, "in place"), ("bf16", 12001, 1400, "apart"), ("bf16", 16384, 1281, "none"),
                                            ("f32", 2051, 1301, "in place"), ("f32", 4097, 1301, "in place"), ("f32", 8192, 1283, "apart")])
