@@ -269,7 +269,8 @@ class ChunkedDecoder:
         positions: with rope_axes, int64 [axes, batch or 1, tokens], every token's position on each axis (default: its number in
         the sequence on all of them).
         optimizer: an optimizer.AdamW over these parameters (of a computed one: over the leaves behind it), whose step is taken
-        with the step's gradients, what .grad held before left out (not taken if a token lies outside the table)."""
+        with the step's gradients, what .grad held before left out (not taken if a token lies outside the table); or
+        another object whose step() takes the gradients from .grad."""
         p = self.p
         B, N = tokens.shape
         dtype, dev = p["emb"].dtype, p["emb"].device
@@ -302,7 +303,7 @@ class ChunkedDecoder:
         for t in p.values():
             t.grad = None
         if optimizer is not None:               # (of computed parameters it holds the leaves, which would add up over the steps)
-            its = {id(t) for t in optimizer.params}
+            its = {id(t) for t in getattr(optimizer, "params", ())}
             for t in leaves_behind(p.values()):
                 if id(t) in its:
                     t.grad = None

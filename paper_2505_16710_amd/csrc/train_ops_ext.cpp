@@ -55,7 +55,7 @@ struct Distances {
     size_t i = 0;
     for (; i < dims.size() && dims[i].first <= width; ++i) width += dims[i].first * dims[i].second;
     for (; i < dims.size(); ++i) {
-      const auto [stride, last] = dims[i];
+      const int64_t stride = dims[i].first, last = dims[i].second;
       auto* at = std::find_if(terms.begin(), terms.end(), [&](const Term& t) { return t.stride == stride; });
       if (at == terms.end()) at = terms.insert(at, Term{stride, 0, 0});
       (sign > 0 ? at->last : at->first) += sign * last;

@@ -220,6 +220,15 @@ def test_updates_of_parameters_with_hooks(bits):
 
 
 @pytest.mark.gpu
+def test_another_optimizer_behind_the_step():
+    """Whatever has a step() that takes .grad."""
+    cfg, p64, params, dec, tok, tgt, pos = _setup(18, 1, 96, torch.float32, **_options("layer", torch.float32))
+    before = {n: t.detach().clone() for n, t in params.items()}
+    _, grads = dec.step(tok.to(DEV), tgt.to(DEV), 32, optimizer=torch.optim.SGD(params.values(), lr=0.5))
+    assert all(torch.equal(params[n].detach(), before[n] - 0.5 * grads[n]) for n in params)
+
+
+@pytest.mark.gpu
 def test_updates_of_leaves_behind_computed_parameters():
     """A matrix computed from a leaf, anew for every step: the optimizer's leaf holds the last step's gradient alone; one that
     the optimizer does not hold adds up, as in backward()."""
