@@ -241,15 +241,18 @@ class RopeAxes:
 
     sections: pairs of each axis, one to four of them, adding up to head_dim / 2.  interleaved: pairs are dealt to the axes in
     turn (else in one run per axis).  own_frequencies: a ladder base^(-k / n) over each axis' n pairs (else one,
-    base^(-2 i / head_dim), over all).  Built once and kept by the program."""
+    base^(-2 i / head_dim), over all).  base: what fp32 makes of it (the attribute), as in the calls with one axis.  Built once
+    and kept by the program."""
 
     def __init__(self, sections, base, interleaved=False, own_frequencies=False):
         self.sections = tuple(int(n) for n in sections)
-        self.base, self.interleaved, self.own_frequencies = float(base), bool(interleaved), bool(own_frequencies)
+        base = float(base)
+        if not 1.0 < base <= 3.4028234663852886e38 or struct.unpack("f", struct.pack("f", base))[0] == 1.0:
+            raise ValueError("base must be finite and above 1 in fp32")
+        self.base = struct.unpack("f", struct.pack("f", base))[0]
+        self.interleaved, self.own_frequencies = bool(interleaved), bool(own_frequencies)
         if not 1 <= len(self.sections) <= 4 or min(self.sections) < 0 or not 4 <= sum(self.sections) <= 128 or sum(self.sections) % 4:
             raise ValueError("sections: one to four numbers of pairs that add up to a multiple of 4, at most 128")
-        if not 1.0 < self.base < float("inf"):
-            raise ValueError("base must be finite and above 1")
         self.head_dim = 2 * sum(self.sections)
         self.packed = struct.pack("=3if4i", len(self.sections), self.interleaved, self.own_frequencies, self.base,
                                   *(self.sections + (0, 0, 0))[:4])

@@ -470,6 +470,14 @@ def test_caches_and_results_that_share_memory():
     assert torch.equal(gk[:, :, 7:17], want[1]) and torch.equal(gv[:, :, 7:17], want[2]) and torch.equal(gk[:, :, 17:], g[:, :, 17:])
 
 
+def test_the_base_is_fp32():
+    for base in (1.00000001, 1e39, 1.0, float("nan")):
+        with pytest.raises(ValueError, match="fp32"):
+            seco.RopeAxes((64,), base)
+    assert seco.RopeAxes((64,), 500000).base == 500000.0
+    assert seco.RopeAxes((64,), 1e6 / 3).base == float(torch.tensor(1e6 / 3)) and seco.RopeAxes((64,), 3.4028234663852886e38).base < math.inf
+
+
 def test_status_codes():
     lib = seco.load_library()
     from paper_2505_16710_amd.binding import SecoDesc
